@@ -242,6 +242,24 @@ int revive_route(revive_ctx* ctx, const void* x, const void* w_router, float* lo
                  int32_t logits_given, int32_t T, int32_t* topk_logical, float* topk_weight,
                  int32_t* topk_phys, revive_stream stream);
 
+/* Gate with a bias for balance.  As revive_route, but experts are chosen by
+ * key_e = score_e + bias_e and weighted by the score alone:
+ *   bias       dev fp32 [E]
+ *   scores     softmax over all E logits (lost experts' included), or elementwise
+ *              sigmoid, in fp32.  The order of the keys is that of fp32 numbers:
+ *              keys closer than their rounding may swap.
+ *   n_group > 1: a group scores the sum of its two best keys above -inf, in fp32.
+ *   topk_weight: the chosen expert's score (without the bias); renormalise != 0:
+ *              over the sum of the chosen scores; then times route_scale.
+ * A NaN key orders nothing: its expert counts as absent while live experts with
+ * numbers are left, in its group's score too, and is chosen after them in
+ * ascending id (its weight is NaN; renormalised, so are its row's).  Bias may be
+ * infinite: -inf puts an expert behind all others, +inf in front of them.
+ * Everything else (mask, ties, replicas, token offset) is revive_route's. */
+int revive_route_biased(revive_ctx* ctx, const void* x, const void* w_router, float* logits,
+                        int32_t logits_given, const float* bias, int32_t renormalise, int32_t T,
+                        int32_t* topk_logical, float* topk_weight, int32_t* topk_phys, revive_stream stream);
+
 /* Microbatches (Sec. 2.2): when x holds rows [first_token, first_token + T) of a
  * larger batch, the replica rule of revive_route uses the token's index in the
  * whole batch, (first_token + t) mod count[e], so that the microbatches choose
@@ -261,6 +279,12 @@ int revive_set_token_offset(revive_ctx* ctx, int64_t first_token);
 int revive_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys, int32_t T,
                     void* x_perm, int32_t* slot_offsets, int32_t* dst_row, int32_t* src_of,
                     revive_stream stream);
+
+/* The indices of revive_dispatch without the row permutation, for an FFN that
+ * reads its rows through src_of (revive_mx_expert_ffn).  Same slot_offsets,
+ * dst_row and src_of. */
+int revive_dispatch_index(revive_ctx* ctx, const int32_t* topk_phys, int32_t T, int32_t* slot_offsets,
+                          int32_t* dst_row, int32_t* src_of, revive_stream stream);
 
 /* revive_dispatch for callers that cannot allocate or bind device memory (code
  * under graph capture set up by someone else, serving loops and harnesses that
@@ -302,6 +326,62 @@ int revive_expert_ffn(revive_ctx* ctx, const void* x_perm, const int32_t* slot_o
 int revive_shared_ffn(revive_ctx* ctx, const void* x, const void* w_sh_gate_up,
                       const void* w_sh_down, void* y_shared, int32_t T, revive_stream stream);
 
+/* ---- microscaled 4-bit floats (MXFP4) -------------------------------------
+ *
+ * A row is cut into blocks of 32 numbers along K.  A block has a scale 2^e, kept
+ * as the byte e + 127, and its numbers are kept as 4-bit codes: sign (8) and
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 (0..7).
+ *   e = clamp(floor(log2(largest magnitude)) - 2, -127, 127); zeros: byte 0
+ *   code = x / 2^e rounded to the nearest, ties to the even code, at most 6
+ * A block that holds an infinity or a NaN gets byte 255 and stands for 32 NaNs.
+ * The four calls need no context; they launch on `stream` of the current device,
+ * allocate nothing and may be captured.  Their errors: revive_last_error(NULL).
+ *
+ * revive_mx_quantize:
+ *   x       dev [rows, K], fp32 or bf16 (dtype), rows ld elements apart
+ *   codes   dev uint8 [rows, 16 * ceil(K/32)], two codes a byte, the lower k in the
+ *           lower half, 16-byte aligned; the last block filled up with zeros
+ *   scales  dev uint8 [rows, ceil(K/32)]
+ * revive_mx_dequantize: the numbers they stand for, [rows, K], fp32 or bf16 (both
+ *   hold them exactly), rows ld elements apart.
+ * K <= 2^24; rows with a stride and an address of whole 16 bytes are faster. */
+int revive_mx_quantize(const void* x, int32_t dtype, int64_t rows, int32_t K, int64_t ld, uint8_t* codes,
+                       uint8_t* scales, revive_stream stream);
+int revive_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype,
+                         void* out, int64_t ld, revive_stream stream);
+
+/* Weights of the 4-bit FFN: codes and scales of an output-major matrix [rows, K]
+ * (K a multiple of 32) into the order in which the kernels read them.
+ * revive_mx_packed_bytes gives the size of `packed` (dev, 16-byte aligned).  Rows
+ * are filled up with zeros to a multiple of 128.  Packed, a matrix is
+ *   codes  [rows/128][ceil(K/128)][8][64][16 bytes]: blocks of 16 rows x 128 K;
+ *          lane l = 0..63 of a block has K 32*(l/16) .. +31 of the block's row l%16
+ *   scales [rows/128][ceil(K/512)][8][64][4 bytes]: byte s of lane l is the scale of
+ *          the lane's 32 numbers in the s-th of the group's four blocks of 128 K
+ * and row m of block b (0..7) of a panel is the matrix' row 32*(b/2) + 8*(m/4) +
+ * 4*(b%2) + m%4 of the panel.  A gate and an up matrix follow each other. */
+int revive_mx_packed_bytes(int32_t rows, int32_t K, size_t* bytes /*host*/);
+int revive_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t K, void* packed,
+                   revive_stream stream);
+
+/* Expert FFN on microscaled 4-bit weights and activations, for bf16 layers.  With
+ * Q the rounding above along a row, for every slot p with rows [slot_offsets[p],
+ * slot_offsets[p+1]):  h = Q(silu(Q(x) G_p) * (Q(x) U_p)),  y = h D_p, fp32 sums, and
+ * the same on all T rows of x for the shared expert when y_shared != NULL.
+ *   x          dev [T, H] bf16: the tokens, not permuted; quantised here, once each
+ *   src_of     dev int32 [N] (revive_dispatch_index): row r is token src_of[r] / k
+ *   w_gate_up  dev table of P dev pointers: packed gate matrix [I, H] followed by
+ *              the packed up matrix;  w_down: packed [H, I].  Entries of slots that
+ *              receive no rows are never dereferenced.
+ *   y_perm     dev [N, H] bf16;  rows beyond slot_offsets[P] are left alone
+ *   w_sh_gate_up, w_sh_down, y_shared [T, H]: shared expert, may be NULL
+ * Outputs and weights are 16-byte aligned.  Uses the whole workspace: not to overlap
+ * with revive_expert_ffn or revive_shared_ffn of the same context. */
+int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, const int32_t* slot_offsets,
+                         const void* const* w_gate_up, const void* const* w_down, void* y_perm,
+                         const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int32_t T,
+                         revive_stream stream);
+
 /* a9 - Combine / E2A (Sec. 2.3): out[t, :] = sum_j topk_weight[t, j] *
  * y_perm[dst_row[t*k + j], :] (+ y_shared[t, :]); fp32 accumulation in
  * ascending j, shared expert last, one rounding to dtype.
@@ -337,6 +417,9 @@ enum {
   REVIVE_K_FFN_SHARED_DOWN,
   REVIVE_K_COMBINE,
   REVIVE_K_EXPERT_COUNTS,
+  REVIVE_K_MX_QUANTIZE,
+  REVIVE_K_MX_GATE_UP,
+  REVIVE_K_MX_DOWN,
   REVIVE_K_COUNT
 };
 

@@ -24,7 +24,7 @@ TORCH_DTYPE = {"fp32": torch.float32, "bf16": torch.bfloat16}
 
 KERNEL_NAMES = ["router_gemm", "route_topk", "dispatch_index",
                 "dispatch_permute", "ffn_tiles", "ffn_gate_up", "ffn_down", "ffn_shared_gate_up",
-                "ffn_shared_down", "combine", "expert_counts"]
+                "ffn_shared_down", "combine", "expert_counts", "mx_quantize", "mx_gate_up", "mx_down"]
 
 
 class ReviveError(RuntimeError):
@@ -79,6 +79,13 @@ def lib() -> C.CDLL:
         "revive_expert_counts": (C.c_int, [vp, vp, i32, vp, vp]),
         "revive_build_map": (C.c_int, [P(Config), vp, vp, vp, vp, vp, P(MapStats)]),
         "revive_route": (C.c_int, [vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]),
+        "revive_route_biased": (C.c_int, [vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp]),
+        "revive_dispatch_index": (C.c_int, [vp, vp, i32, vp, vp, vp, vp]),
+        "revive_mx_quantize": (C.c_int, [vp, i32, C.c_int64, i32, C.c_int64, vp, vp, vp]),
+        "revive_mx_dequantize": (C.c_int, [vp, vp, C.c_int64, i32, i32, vp, C.c_int64, vp]),
+        "revive_mx_packed_bytes": (C.c_int, [i32, i32, P(sz)]),
+        "revive_mx_pack": (C.c_int, [vp, vp, i32, i32, vp, vp]),
+        "revive_mx_expert_ffn": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
         "revive_dispatch": (C.c_int, [vp, vp, vp, i32, vp, vp, vp, vp, vp]),
         "revive_set_token_offset": (C.c_int, [vp, C.c_int64]),
         "revive_get_rank_map": (C.c_int, [vp, vp, vp]),
@@ -111,6 +118,8 @@ EXPORTS = ["revive_create", "revive_destroy", "revive_workspace_bytes", "revive_
            "revive_set_placement", "revive_update_map", "revive_update_map_experts", "revive_get_map", "revive_build_map",
            "revive_build_map_experts", "revive_compact_ranks", "revive_mask_every_nth", "revive_mask_most_activated", "revive_expert_counts",
            "revive_get_rank_map", "revive_rank_offsets", "revive_set_token_offset",
+           "revive_route_biased", "revive_dispatch_index", "revive_mx_quantize", "revive_mx_dequantize", "revive_mx_packed_bytes",
+           "revive_mx_pack", "revive_mx_expert_ffn",
            "revive_route", "revive_dispatch", "revive_dispatch_static", "revive_expert_ffn", "revive_shared_ffn", "revive_combine",
            "revive_graph_begin", "revive_graph_end", "revive_graph_launch", "revive_graph_exec_id",
            "revive_graph_destroy", "revive_set_kernel_timing", "revive_kernel_time",
@@ -225,6 +234,103 @@ def unpack_expert(w_gate_up: torch.Tensor, w_down: torch.Tensor, H: int, I: int)
     return w_gate_up[:I].t(), w_gate_up[I:].t(), w_down.t()
 
 
+# ---- microscaled 4-bit floats --------------------------------------------------------------------
+
+MX_BLOCK = 32
+
+
+def _current_stream(stream: Optional[torch.cuda.Stream]) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    # without the Stream object that torch.cuda.current_stream() makes: that took 2.6 us of each of the four calls of an
+    # eager step (64 tokens, H = 256, fp32: 33 -> 24 us)
+    return _raw_stream(torch.cuda.current_device())
+
+
+def _check_free(rc: int):
+    """Status of a call that has no context."""
+    if rc != 0:
+        raise ReviveError(rc, lib().revive_last_error(None).decode())
+
+
+def _mx_dtype(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return DTYPE["bf16"]
+    if t.dtype == torch.float32:
+        return DTYPE["fp32"]
+    raise TypeError(f"microscaled numbers are made of and into float32 and bfloat16, not {t.dtype}")
+
+
+def _mx_form(codes: torch.Tensor, scales: torch.Tensor):
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
+        raise ValueError("codes and scales are uint8 matrices")
+    if codes.shape != (scales.shape[0], 16 * scales.shape[1]) or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)}: contiguous [rows, 16 n] and [rows, n] expected")
+
+
+def mx_quantize(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """revive_mx_quantize: x [rows, K] fp32 or bf16 (rows may be strided) -> (codes [rows, 16 n], scales [rows, n]), n =
+    ceil(K / 32) blocks of 32."""
+    dtype = _mx_dtype(x)
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+        raise ValueError("x is a matrix whose rows are contiguous and do not overlap")
+    rows, K = x.shape
+    n = -(-K // MX_BLOCK)
+    if out is None:
+        out = (torch.empty(rows, 16 * n, dtype=torch.uint8, device=x.device), torch.empty(rows, n, dtype=torch.uint8, device=x.device))
+    codes, scales = out
+    _mx_form(codes, scales)
+    if scales.shape != (rows, n):
+        raise ValueError(f"scales {tuple(scales.shape)}: {(rows, n)} expected")
+    _check_free(lib().revive_mx_quantize(x.data_ptr(), dtype, rows, K, x.stride(0) if rows > 1 else K, codes.data_ptr(),
+                                         scales.data_ptr(), _current_stream(stream)))
+    return codes, scales
+
+
+def mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, K: Optional[int] = None, dtype=torch.bfloat16, out=None,
+                  stream=None) -> torch.Tensor:
+    """revive_mx_dequantize: the numbers that codes and scales stand for, [rows, K] (default: all of the blocks, or out's)."""
+    _mx_form(codes, scales)
+    rows, n = scales.shape
+    if out is None:
+        out = torch.empty(rows, MX_BLOCK * n if K is None else K, dtype=dtype, device=codes.device)
+    if out.dim() != 2 or out.shape[0] != rows or -(-out.shape[1] // MX_BLOCK) != n or (K is not None and out.shape[1] != K):
+        raise ValueError(f"out {tuple(out.shape)} does not fit {rows} rows of {n} blocks")
+    if (out.shape[1] > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < out.shape[1]):
+        raise ValueError("out is a matrix whose rows are contiguous and do not overlap")
+    _check_free(lib().revive_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, out.shape[1], _mx_dtype(out), out.data_ptr(),
+                                           out.stride(0) if rows > 1 else out.shape[1], _current_stream(stream)))
+    return out
+
+
+def mx_packed_bytes(rows: int, K: int) -> int:
+    n = C.c_size_t()
+    _check_free(lib().revive_mx_packed_bytes(rows, K, C.byref(n)))
+    return n.value
+
+
+def mx_pack(codes: torch.Tensor, scales: torch.Tensor, out=None, stream=None) -> torch.Tensor:
+    """revive_mx_pack: an output-major weight matrix' codes and scales -> uint8 in the order that the 4-bit FFN reads."""
+    _mx_form(codes, scales)
+    rows, K = scales.shape[0], scales.shape[1] * MX_BLOCK
+    n = mx_packed_bytes(rows, K)
+    if out is None:
+        out = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    if out.dtype != torch.uint8 or out.numel() != n or not out.is_contiguous():
+        raise ValueError(f"out: {n} contiguous bytes expected")
+    _check_free(lib().revive_mx_pack(codes.data_ptr(), scales.data_ptr(), rows, K, out.data_ptr(), _current_stream(stream)))
+    return out
+
+
+def mx_pack_expert(gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Math-layout expert matrices (gate/up [H, I], down [I, H], fp32 or bf16) -> (w_gate_up, w_down), quantised along each
+    product's K and packed."""
+    g, u, d = (mx_pack(*mx_quantize(w.t().contiguous())) for w in (gate, up, down))
+    return torch.cat([g, u]), d
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -251,6 +357,7 @@ class ReviveLayer:
             self.workspace = torch.empty(max(256, nbytes.value), dtype=torch.uint8, device=self.device)
             self._check(self.L.revive_bind_workspace(self._ctx, self.workspace.data_ptr(), self.workspace.numel()))
         self._w_tabs = None
+        self._mx_tabs = None
         self._graphs: List[C.c_void_p] = []
 
     # -- plumbing --------------------------------------------------------------------------
@@ -258,15 +365,7 @@ class ReviveLayer:
         if rc != 0:
             raise ReviveError(rc, self.L.revive_last_error(self._ctx).decode())
 
-    @staticmethod
-    def _stream(stream: Optional[torch.cuda.Stream]) -> int:
-        if stream is not None:
-            return stream.cuda_stream
-        if _raw_stream is None:
-            return torch.cuda.current_stream().cuda_stream
-        # without the Stream object that torch.cuda.current_stream() makes: that took 2.6 us of each of the four calls of an
-        # eager step (64 tokens, H = 256, fp32: 33 -> 24 us)
-        return _raw_stream(torch.cuda.current_device())
+    _stream = staticmethod(_current_stream)
 
     def close(self):
         if self._ctx:
@@ -358,6 +457,17 @@ class ReviveLayer:
         dn_tab = torch.tensor([0 if t is None else t.data_ptr() for t in w_down], dtype=torch.int64)
         self._w_tabs = (gu_tab.to(self.device), dn_tab.to(self.device))
 
+    def set_mx_expert_weights(self, w_gate_up: Sequence[Optional[torch.Tensor]], w_down: Sequence[Optional[torch.Tensor]]):
+        """Per-slot packed 4-bit weights (mx_pack_expert; lists of P tensors, None for empty slots) -> device pointer tables."""
+        assert len(w_gate_up) == self.P and len(w_down) == self.P
+        n_gu, n_dn = 2 * mx_packed_bytes(self.cfg.I, self.cfg.H), mx_packed_bytes(self.cfg.H, self.cfg.I)
+        for w, n in [(w, n_gu) for w in w_gate_up] + [(w, n_dn) for w in w_down]:
+            if w is not None:
+                assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.data_ptr() % 16 == 0
+        self._mx_keep = (list(w_gate_up), list(w_down))
+        self._mx_tabs = tuple(torch.tensor([0 if w is None else w.data_ptr() for w in ws], dtype=torch.int64).to(self.device)
+                              for ws in (w_gate_up, w_down))
+
     # -- data path -------------------------------------------------------------------------
     def route(self, x, w_router, T: int, logits=None, logits_given=False, out=None, stream=None):
         k = self.cfg.k
@@ -370,6 +480,29 @@ class ReviveLayer:
         self._check(self.L.revive_route(self._ctx, _ptr(x), _ptr(w_router), _ptr(logits), int(bool(logits_given)), T,
                                         _ptr(top_l), _ptr(top_w), _ptr(top_p), self._stream(stream)))
         return logits, top_l, top_w, top_p
+
+    def route_biased(self, x, w_router, bias, T: int, renormalise=True, logits=None, logits_given=False, out=None, stream=None):
+        """revive_route_biased: experts chosen by score + bias (fp32 [E]), weighted by the score."""
+        k = self.cfg.k
+        if logits is None:
+            logits = self.empty(T, self.cfg.E, dtype=torch.float32)
+        if out is None:
+            out = (self.empty(T, k, dtype=torch.int32), self.empty(T, k, dtype=torch.float32),
+                   self.empty(T, k, dtype=torch.int32))
+        top_l, top_w, top_p = out
+        self._check(self.L.revive_route_biased(self._ctx, _ptr(x), _ptr(w_router), _ptr(logits), int(bool(logits_given)), _ptr(bias),
+                                               int(bool(renormalise)), T, _ptr(top_l), _ptr(top_w), _ptr(top_p), self._stream(stream)))
+        return logits, top_l, top_w, top_p
+
+    def dispatch_index(self, topk_phys, T: int, out=None, stream=None):
+        """revive_dispatch_index: (slot_offsets, dst_row, src_of) without permuted rows."""
+        N = T * self.cfg.k
+        if out is None:
+            out = (self.empty(self.P + 1, dtype=torch.int32), self.empty(N, dtype=torch.int32), self.empty(N, dtype=torch.int32))
+        slot_offsets, dst_row, src_of = out
+        self._check(self.L.revive_dispatch_index(self._ctx, _ptr(topk_phys), T, _ptr(slot_offsets), _ptr(dst_row), _ptr(src_of),
+                                                 self._stream(stream)))
+        return slot_offsets, dst_row, src_of
 
     def dispatch(self, x, topk_phys, T: int, out=None, stream=None, static_scratch=False):
         """revive_dispatch, or with static_scratch revive_dispatch_static (which needs `out`: it is
@@ -398,6 +531,19 @@ class ReviveLayer:
                                              _ptr(w_sh_gate_up) if use_shared else None,
                                              _ptr(w_sh_down) if use_shared else None,
                                              _ptr(y_shared) if use_shared else None, T, self._stream(stream)))
+        return y_perm, y_shared
+
+    def mx_expert_ffn(self, x, src_of, slot_offsets, T: int, w_sh_gate_up=None, w_sh_down=None, out=None, stream=None):
+        """revive_mx_expert_ffn: (y_perm, y_shared) of the 4-bit experts; x [T, H] as it came, rows found through src_of."""
+        assert self._mx_tabs is not None, "set_mx_expert_weights first"
+        use_shared = w_sh_gate_up is not None
+        if out is None:
+            out = (self.empty(T * self.cfg.k, self.cfg.H), self.empty(T, self.cfg.H) if use_shared else None)
+        y_perm, y_shared = out
+        self._check(self.L.revive_mx_expert_ffn(self._ctx, _ptr(x), _ptr(src_of), _ptr(slot_offsets), _ptr(self._mx_tabs[0]),
+                                                _ptr(self._mx_tabs[1]), _ptr(y_perm), _ptr(w_sh_gate_up) if use_shared else None,
+                                                _ptr(w_sh_down) if use_shared else None, _ptr(y_shared) if use_shared else None, T,
+                                                self._stream(stream)))
         return y_perm, y_shared
 
     def shared_ffn(self, x, w_sh_gate_up, w_sh_down, T: int, out=None, stream=None):

@@ -9,7 +9,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "librevive.so")
-SOURCES = ["api.hip", "map_host.cpp", "route.hip", "dispatch.hip", "ffn.hip", "combine.hip", "study.hip"]
+SOURCES = ["api.hip", "map_host.cpp", "route.hip", "dispatch.hip", "ffn.hip", "combine.hip", "study.hip",
+           "route_biased.hip", "mx_quant.hip", "mx_ffn.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

@@ -5,6 +5,7 @@
 #include <utility>
 
 #include "ctx.hpp"
+#include "mx.hpp"
 
 namespace revive {
 
@@ -114,6 +115,19 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
   w.off_h_shared = off;
   off = align_up(off + ctx->elem * static_cast<size_t>(c.T_max) * c.I_shared, 256);
   w.bytes = off;
+  if (c.dtype == REVIVE_DTYPE_BF16) {
+    off = w.off_h;
+    auto codes_and_scales = [&off](int64_t rows, int K, size_t& codes, size_t& scales) {
+      codes = off;
+      off = align_up(off + static_cast<size_t>(rows) * mx_steps(K) * (kMxStep / 2), 256);
+      scales = off;
+      off = align_up(off + static_cast<size_t>(rows) * mx_scale_row(K), 256);
+    };
+    codes_and_scales(c.T_max, c.H, w.off_mx_x, w.off_mx_x_scales);
+    codes_and_scales(N_max, c.I, w.off_mx_h, w.off_mx_h_scales);
+    codes_and_scales(c.T_max, c.I_shared, w.off_mx_h_shared, w.off_mx_h_shared_scales);
+    w.bytes = std::max(w.bytes, off);
+  }
 
   int rc = check_hip(nullptr, hipGetDevice(&ctx->device), "hipGetDevice");
   if (rc == REVIVE_OK) rc = check_hip(nullptr, hipMalloc(reinterpret_cast<void**>(&ctx->d_map), m.bytes), "hipMalloc(map)");
@@ -270,6 +284,50 @@ int revive_route(revive_ctx* ctx, const void* x, const void* w_router, float* lo
     if (rc != REVIVE_OK) return rc;
   }
   return launch_route_topk(ctx, logits, T, topk_logical, topk_weight, topk_phys, s);
+}
+
+int revive_route_biased(revive_ctx* ctx, const void* x, const void* w_router, float* logits, int32_t logits_given, const float* bias,
+                        int32_t renormalise, int32_t T, int32_t* topk_logical, float* topk_weight, int32_t* topk_phys, revive_stream stream) {
+  int rc = check_call(ctx, "revive_route_biased", T, false);
+  if (rc != REVIVE_OK) return rc;
+  if (!ctx->map_set) return fail(ctx, REVIVE_ESTATE, "revive_route_biased: call revive_update_map first");
+  if (!logits || !bias || !topk_logical || !topk_weight || !topk_phys) return fail(ctx, REVIVE_EINVAL, "revive_route_biased: null output, logits or bias");
+  if (!logits_given && (!x || !w_router)) return fail(ctx, REVIVE_EINVAL, "revive_route_biased: x and w_router are required unless logits are given");
+  if (T == 0) return REVIVE_OK;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!logits_given) {
+    rc = launch_router_gemm(ctx, x, w_router, logits, T, s);
+    if (rc != REVIVE_OK) return rc;
+  }
+  return launch_route_biased(ctx, logits, bias, renormalise != 0, T, topk_logical, topk_weight, topk_phys, s);
+}
+
+int revive_dispatch_index(revive_ctx* ctx, const int32_t* topk_phys, int32_t T, int32_t* slot_offsets, int32_t* dst_row, int32_t* src_of,
+                          revive_stream stream) {
+  int rc = check_call(ctx, "revive_dispatch_index", T, true);
+  if (rc != REVIVE_OK) return rc;
+  if (!slot_offsets) return fail(ctx, REVIVE_EINVAL, "revive_dispatch_index: null slot_offsets");
+  if (T > 0 && (!topk_phys || !dst_row || !src_of)) return fail(ctx, REVIVE_EINVAL, "revive_dispatch_index: null argument");
+  return launch_dispatch_index(ctx, topk_phys, T, slot_offsets, dst_row, src_of, static_cast<hipStream_t>(stream));
+}
+
+int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, const int32_t* slot_offsets, const void* const* w_gate_up,
+                         const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int32_t T,
+                         revive_stream stream) {
+  int rc = check_call(ctx, "revive_mx_expert_ffn", T, true);
+  if (rc != REVIVE_OK) return rc;
+  if (ctx->cfg.dtype != REVIVE_DTYPE_BF16) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: the layer must be bf16");
+  if (T == 0) return REVIVE_OK;
+  if (!x || !src_of || !slot_offsets || !w_gate_up || !w_down || !y_perm) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: null argument");
+  if (y_shared) {
+    if (ctx->cfg.I_shared == 0) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: y_shared given but the layer has no shared expert");
+    if (!w_sh_gate_up || !w_sh_down) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: the shared expert needs both weight matrices");
+  }
+  for (const void* p : {static_cast<const void*>(y_perm), static_cast<const void*>(y_shared), w_sh_gate_up, w_sh_down})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: outputs and weights must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(x) % 2 != 0) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: x is not aligned to its elements");
+  return launch_mx_expert_ffn(ctx, x, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T,
+                              static_cast<hipStream_t>(stream));
 }
 
 int revive_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys, int32_t T, void* x_perm,
@@ -437,7 +495,8 @@ int revive_reset_kernel_times(revive_ctx* ctx) {
 const char* revive_kernel_name(int32_t kernel) {
   static const char* names[REVIVE_K_COUNT] = {
       "router_gemm", "route_topk", "dispatch_index", "dispatch_permute",
-      "ffn_tiles", "ffn_gate_up", "ffn_down", "ffn_shared_gate_up", "ffn_shared_down", "combine", "expert_counts"};
+      "ffn_tiles", "ffn_gate_up", "ffn_down", "ffn_shared_gate_up", "ffn_shared_down", "combine", "expert_counts",
+      "mx_quantize", "mx_gate_up", "mx_down"};
   return kernel >= 0 && kernel < REVIVE_K_COUNT ? names[kernel] : "?";
 }
 

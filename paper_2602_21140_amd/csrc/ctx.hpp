@@ -68,6 +68,10 @@ struct Workspace {
   size_t off_tile_count;  // int32 [4]
   size_t off_h;           // dtype [N_max * I]
   size_t off_h_shared;    // dtype [T_max * I_shared]
+  // the 4-bit FFN's, over off_h and off_h_shared: a context runs one FFN at a time
+  size_t off_mx_x, off_mx_x_scales;                // x: codes [T_max][steps of H][64], scales [T_max][mx_scale_row(H)]
+  size_t off_mx_h, off_mx_h_scales;                // h: codes [steps of I][N_max][64], scales [N_max][mx_scale_row(I)]
+  size_t off_mx_h_shared, off_mx_h_shared_scales;  // the shared expert's h
   size_t bytes;
 };
 
@@ -164,6 +168,12 @@ int launch_expert_ffn(revive_ctx*, const void* x_perm, const int32_t* slot_offse
                       const void* w_sh_down, void* y_shared, int T, hipStream_t);
 int launch_shared_ffn(revive_ctx*, const void* x, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int T,
                       hipStream_t);
+int launch_dispatch_index(revive_ctx*, const int32_t* topk_phys, int T, int32_t* slot_offsets, int32_t* dst_row, int32_t* src_of, hipStream_t);
+int launch_route_biased(revive_ctx*, const float* logits, const float* bias, bool renormalise, int T, int32_t* topk_logical, float* topk_weight,
+                        int32_t* topk_phys, hipStream_t);
+int launch_mx_expert_ffn(revive_ctx*, const void* x, const int32_t* src_of, const int32_t* slot_offsets, const void* const* w_gate_up,
+                         const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int T,
+                         hipStream_t);
 int launch_expert_counts(revive_ctx*, const int32_t* topk_logical, int T, int64_t* counts, hipStream_t);
 int launch_combine(revive_ctx*, const void* y_perm, const int32_t* dst_row, const float* topk_weight,
                    const void* y_shared, int T, void* out, hipStream_t);

@@ -266,6 +266,20 @@ __global__ __launch_bounds__(kThreads) void dispatch_small_kernel(const uint4* _
   }
 }
 
+// Destinations alone, a thread per routed row: what dispatch_permute_kernel does without the rows.
+__global__ __launch_bounds__(kThreads) void dispatch_place_kernel(const int32_t* __restrict__ topk_phys, int N, int P, const int32_t* __restrict__ block_base,
+                                                                  const int32_t* __restrict__ slot_offsets, int32_t* __restrict__ dst_row,
+                                                                  int32_t* __restrict__ src_of) {
+  const int i = blockIdx.x * kThreads + threadIdx.x;
+  if (i >= N) return;
+  const int r = dst_row[i];
+  if (r < 0) return;  // dropped: its destination stays -1
+  const int p = topk_phys[i];
+  const int d = slot_offsets[p] + block_base[static_cast<int64_t>(i / kChunk) * P + p] + r;
+  src_of[d] = i;
+  dst_row[i] = d;
+}
+
 // Compacted rank segments (Sec. 3.5): after the failed ranks have left the communication domain the
 // survivors are renumbered 0 .. n_live-1 in their old order; segment l of the permuted buffer is the
 // rows of the rank that now holds logical rank l.  Failed ranks received no rows, so the compacted
@@ -300,10 +314,10 @@ static int run_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys
   const int P = ctx->P;
   const int N = T * c.k;
   const int n_chunks = ceil_div(N, kChunk);
-  const int row_words = static_cast<int>(c.H * ctx->elem / 16);
+  const int row_words = x_perm ? static_cast<int>(c.H * ctx->elem / 16) : 0;  // x_perm null: indices alone
   if (N <= kSmallRows) {
     KernelTimer timer(ctx, REVIVE_K_DISPATCH_PERMUTE, stream);
-    hipLaunchKernelGGL(dispatch_small_kernel, dim3(T + 1, ceil_div(row_words, kThreads)), dim3(kThreads), 0, stream,
+    hipLaunchKernelGGL(dispatch_small_kernel, dim3(T + 1, x_perm ? ceil_div(row_words, kThreads) : 1), dim3(kThreads), 0, stream,
                        static_cast<const uint4*>(x), topk_phys, T, c.k, P, row_words, slot_offsets, dst_row, src_of,
                        static_cast<uint4*>(x_perm));
     return check_hip(ctx, hipGetLastError(), "dispatch_small launch");
@@ -317,6 +331,10 @@ static int run_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys
     REVIVE_HIP(ctx, hipGetLastError());
   }
   KernelTimer timer(ctx, REVIVE_K_DISPATCH_PERMUTE, stream);
+  if (!x_perm) {
+    hipLaunchKernelGGL(dispatch_place_kernel, dim3(ceil_div(N, kThreads)), dim3(kThreads), 0, stream, topk_phys, N, P, block_hist, slot_offsets, dst_row, src_of);
+    return check_hip(ctx, hipGetLastError(), "dispatch_place launch");
+  }
   hipLaunchKernelGGL(dispatch_permute_kernel, dim3(T), dim3(kThreads), 0, stream, static_cast<const uint4*>(x), topk_phys, c.k, P,
                      block_hist, slot_offsets, row_words, dst_row, src_of, static_cast<uint4*>(x_perm));
   return check_hip(ctx, hipGetLastError(), "dispatch_permute launch");
@@ -327,6 +345,10 @@ int launch_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys, in
   return run_dispatch(ctx, x, topk_phys, T, x_perm, slot_offsets, dst_row, src_of,
                       reinterpret_cast<int32_t*>(ctx->d_ws + ctx->ws.off_block_hist),
                       reinterpret_cast<unsigned int*>(ctx->d_ws + ctx->ws.off_ticket), stream);
+}
+
+int launch_dispatch_index(revive_ctx* ctx, const int32_t* topk_phys, int T, int32_t* slot_offsets, int32_t* dst_row, int32_t* src_of, hipStream_t stream) {
+  return launch_dispatch(ctx, nullptr, topk_phys, T, nullptr, slot_offsets, dst_row, src_of, stream);
 }
 
 // ---- dispatch without any allocation: the scratch is a static device array ---------------------

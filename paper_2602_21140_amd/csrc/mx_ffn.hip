@@ -1,0 +1,90 @@
+// Grouped SwiGLU expert FFN on microscaled 4-bit weights and activations.
+//
+// Paper: Sec. 2.1 (each expert acts as an FFN).  With Q the rounding of mx.hpp, every slot p with rows
+// [slot_offsets[p], slot_offsets[p+1]) computes h = Q(silu(Q(x) G_p) * (Q(x) U_p)), y = h D_p, and the shared expert the same on
+// all tokens.  x is quantised once per token; a routed row reads its token's codes through src_of, so that dispatch need not
+// copy rows.  Slots without rows produce no tile and their weights are never read.
+#include "mx_quant.hpp"
+#include "mx_stream.hpp"
+
+namespace revive {
+
+namespace {
+
+struct MxFfn {
+  const int32_t* src_of; const int32_t* slot_offsets; const void* const* w_gate_up; const void* const* w_down; void* y_perm;
+  const void* w_sh_gate_up; const void* w_sh_down; void* y_shared;
+  int N, T;  // routed rows, rows of the shared expert (0: none)
+};
+
+// One of the FFN's two products on `rows` rows.
+template <int EPI>
+MxProblem mx_problem(const revive_ctx* ctx, const MxFfn& f, bool shared, int tile_m, int tile_n) {
+  const revive_config& c = ctx->cfg;
+  const Workspace& w = ctx->ws;
+  const int I = shared ? c.I_shared : c.I, rows = shared ? f.T : f.N;
+  uint8_t* h = ctx->d_ws + (shared ? w.off_mx_h_shared : w.off_mx_h);
+  uint8_t* h_scales = ctx->d_ws + (shared ? w.off_mx_h_shared_scales : w.off_mx_h_scales);
+  MxProblem p{};
+  p.n_out = EPI == EPI_H ? I : c.H;
+  p.K = EPI == EPI_H ? c.H : I;
+  p.b_codes = mx_packed_codes(p.n_out, p.K);
+  if (EPI == EPI_H) {
+    p.A = ctx->d_ws + w.off_mx_x;
+    p.a_row = mx_steps(c.H) * (kMxStep / 2); p.a_step = kMxStep / 2;
+    p.A_scales = ctx->d_ws + w.off_mx_x_scales;
+    p.src_of = shared ? nullptr : f.src_of; p.k = c.k;
+    p.b_half = mx_packed_bytes(I, c.H);
+    p.H = h; p.H_scales = h_scales; p.h_rows = rows;
+  } else {
+    p.A = h;
+    p.a_row = kMxStep / 2; p.a_step = static_cast<int64_t>(rows) * (kMxStep / 2);
+    p.A_scales = h_scales;
+    p.Y = static_cast<uint16_t*>(shared ? f.y_shared : f.y_perm);
+  }
+  if (shared) p.B_one = EPI == EPI_H ? f.w_sh_gate_up : f.w_sh_down;
+  else p.B_tab = EPI == EPI_H ? f.w_gate_up : f.w_down;
+  p.n_col_tiles = ceil_div(EPI == EPI_H ? static_cast<int>(mx_up(I, kMxPanel)) : c.H, tile_n);
+  const int used = f.N < ctx->P ? f.N : ctx->P;  // slots that can hold a row
+  const int m_tiles = shared ? ceil_div(rows, tile_m) : rows / tile_m + used;
+  p.blocks = m_tiles * p.n_col_tiles;
+  if (!shared) p.blocks = ceil_div(p.blocks, 8) * 8;
+  p.M = rows;
+  return p;
+}
+
+template <int EPI>
+MxArgs mx_args(const revive_ctx* ctx, const MxFfn& f, int tile_m, int tile_n) {
+  MxArgs a{};
+  a.slot_offsets = f.slot_offsets;
+  a.P = ctx->P;
+  a.grouped = mx_problem<EPI>(ctx, f, false, tile_m, tile_n);
+  if (f.T > 0) a.dense = mx_problem<EPI>(ctx, f, true, tile_m, tile_n);
+  return a;
+}
+
+template <int TMX, int W, int NW>
+int mx_stream_ffn(revive_ctx* ctx, const MxFfn& f, hipStream_t stream) {
+  {
+    KernelTimer timer(ctx, REVIVE_K_MX_GATE_UP, stream);
+    const int rc = launch_mx_stream<TMX, W, NW, EPI_H>(ctx, mx_args<EPI_H>(ctx, f, 16 * TMX, NW * W * 8), stream);
+    if (rc != REVIVE_OK) return rc;
+  }
+  KernelTimer timer(ctx, REVIVE_K_MX_DOWN, stream);
+  return launch_mx_stream<TMX, W, NW, EPI_Y>(ctx, mx_args<EPI_Y>(ctx, f, 16 * TMX, NW * W * 16), stream);
+}
+
+}  // namespace
+
+int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, const int32_t* slot_offsets, const void* const* w_gate_up,
+                         const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int T,
+                         hipStream_t stream) {
+  const revive_config& c = ctx->cfg;
+  const Workspace& w = ctx->ws;
+  const int rc = launch_mx_quantize_tiled(ctx, x, T, c.H, ctx->d_ws + w.off_mx_x, ctx->d_ws + w.off_mx_x_scales, stream);
+  if (rc != REVIVE_OK) return rc;
+  const MxFfn f{src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * c.k, y_shared ? T : 0};
+  return mx_stream_ffn<4, 4, 4>(ctx, f, stream);
+}
+
+}  // namespace revive
