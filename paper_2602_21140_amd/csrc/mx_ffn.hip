@@ -6,6 +6,7 @@
 // copy rows.  Slots without rows produce no tile and their weights are never read.
 #include "mx_quant.hpp"
 #include "mx_stream.hpp"
+#include "mx_tile.hpp"
 
 namespace revive {
 
@@ -48,7 +49,7 @@ MxProblem mx_problem(const revive_ctx* ctx, const MxFfn& f, bool shared, int til
   const int used = f.N < ctx->P ? f.N : ctx->P;  // slots that can hold a row
   const int m_tiles = shared ? ceil_div(rows, tile_m) : rows / tile_m + used;
   p.blocks = m_tiles * p.n_col_tiles;
-  if (!shared) p.blocks = ceil_div(p.blocks, 8) * 8;
+  p.blocks = ceil_div(p.blocks, 8) * 8;
   p.M = rows;
   return p;
 }
@@ -74,6 +75,16 @@ int mx_stream_ffn(revive_ctx* ctx, const MxFfn& f, hipStream_t stream) {
   return launch_mx_stream<TMX, W, NW, EPI_Y>(ctx, mx_args<EPI_Y>(ctx, f, 16 * TMX, NW * W * 16), stream);
 }
 
+int mx_tile_ffn(revive_ctx* ctx, const MxFfn& f, hipStream_t stream) {
+  {
+    KernelTimer timer(ctx, REVIVE_K_MX_GATE_UP, stream);
+    const int rc = launch_mx_tile<EPI_H>(ctx, mx_args<EPI_H>(ctx, f, kMxTile, kMxPanel), stream);
+    if (rc != REVIVE_OK) return rc;
+  }
+  KernelTimer timer(ctx, REVIVE_K_MX_DOWN, stream);
+  return launch_mx_tile<EPI_Y>(ctx, mx_args<EPI_Y>(ctx, f, kMxTile, 2 * kMxPanel), stream);
+}
+
 }  // namespace
 
 int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, const int32_t* slot_offsets, const void* const* w_gate_up,
@@ -84,6 +95,8 @@ int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
   const int rc = launch_mx_quantize_tiled(ctx, x, T, c.H, ctx->d_ws + w.off_mx_x, ctx->d_ws + w.off_mx_x_scales, stream);
   if (rc != REVIVE_OK) return rc;
   const MxFfn f{src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * c.k, y_shared ? T : 0};
+  // The tiles address a row of x by 32 bits.
+  if (f.N > 64 * ctx->P && static_cast<int64_t>(T) * mx_steps(c.H) * (kMxStep / 2) < (1ll << 32)) return mx_tile_ffn(ctx, f, stream);
   return mx_stream_ffn<4, 4, 4>(ctx, f, stream);
 }
 

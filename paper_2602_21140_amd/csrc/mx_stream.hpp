@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "ctx.hpp"
+#include "gemm_bf16.hpp"
 #include "mx.hpp"
 #include "row_tiles.hpp"
 
@@ -53,16 +54,6 @@ typedef const __attribute__((address_space(1))) uint32_t* mx_gptr1;
 __device__ __forceinline__ mx_u32x4 mx_load16(const uint8_t* p) { return *reinterpret_cast<mx_gptr>(reinterpret_cast<uintptr_t>(p)); }
 __device__ __forceinline__ uint32_t mx_load4(const uint8_t* p) { return *reinterpret_cast<mx_gptr1>(reinterpret_cast<uintptr_t>(p)); }
 
-// silu(z) = z / (1 + exp(-z)); the hardware's reciprocal is off by an ulp, and exp is +inf where the product is -0.
-__device__ __forceinline__ float mx_silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
-
-__device__ __forceinline__ uint32_t mx_pack_bf16(float lo, float hi) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const f32x2 v = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
 // The lane's eight columns of gate and up of one row, of a block of 32 columns that the lanes l, l ^ 16, l ^ 32, l ^ 48 share
 // -> a word of codes, and the block's scale byte.
 __device__ __forceinline__ uint32_t mx_swiglu_codes(const mx_f32x4& g0, const mx_f32x4& g1, const mx_f32x4& u0, const mx_f32x4& u1, uint32_t& byte) {
@@ -70,7 +61,7 @@ __device__ __forceinline__ uint32_t mx_swiglu_codes(const mx_f32x4& g0, const mx
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i] = i < 4 ? mx_silu(g0[i & 3]) * u0[i & 3] : mx_silu(g1[i & 3]) * u1[i & 3];
+    v[i] = i < 4 ? silu_f32(g0[i & 3]) * u0[i & 3] : silu_f32(g1[i & 3]) * u1[i & 3];
     m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
   }
   m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
@@ -98,6 +89,7 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     n_idx = b - m_idx * g.n_col_tiles;
     row_begin = m_idx * (16 * TMX);
     row_end = min(g.M, row_begin + 16 * TMX);
+    if (row_begin >= row_end) return;  // the grid is filled up to a multiple of 8
     B = static_cast<const uint8_t*>(g.B_one);
     once = g.M <= 16 * TMX;
   } else {
@@ -238,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
           const int col = set * 32 + kb * 8;
           if (row >= row_end || col >= g.n_out) continue;
           const mx_f32x4 &v0 = acc[2 * p][i], &v1 = acc[2 * p + 1][i];
-          const mx_u32x4 o = {mx_pack_bf16(v0[0], v0[1]), mx_pack_bf16(v0[2], v0[3]), mx_pack_bf16(v1[0], v1[1]), mx_pack_bf16(v1[2], v1[3])};
+          const mx_u32x4 o = {pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
           *reinterpret_cast<mx_u32x4*>(g.Y + static_cast<int64_t>(row) * g.n_out + col) = o;
         }
       }
