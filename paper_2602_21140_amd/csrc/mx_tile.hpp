@@ -51,7 +51,10 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, kb = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const int KT = mx_steps(g.K), NG = mx_groups(g.K);
+  const int KR = mx_steps(g.K), NG = mx_groups(g.K);
+  // Whole groups: steps past K repeat the last one with scales of 2^-127 on both sides, and products of 2^-249 at most add
+  // nothing to a sum in fp32.
+  const int KT = NG * 4;
   const int rows = row_end - row_begin;
 
   // ---- copies.  Of a step: two blocks of 16 weight rows and two of 16 rows of A per wavefront; of a group's scales: 64 rows
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
   auto matrix = [&](int half) {  // where panel `half` of this workgroup begins: its first weights, and its first scales
     const int panel = EPI == EPI_H ? n_idx : min(n_idx * 2 + half, n_panels - 1);
     const uint8_t* m = B + (EPI == EPI_H && half ? g.b_half : 0);
-    struct { const uint8_t *codes, *scales; } p = {m + static_cast<int64_t>(panel) * KT * kMxPanelStep, m + g.b_codes + static_cast<int64_t>(panel) * NG * kMxPanelScales};
+    struct { const uint8_t *codes, *scales; } p = {m + static_cast<int64_t>(panel) * KR * kMxPanelStep, m + g.b_codes + static_cast<int64_t>(panel) * NG * kMxPanelScales};
     return p;
   };
   uint32_t a_off[2];
@@ -94,12 +97,13 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
   // Step kt into stage PH = kt % 4; with the first step of a group, its scales.
   auto copy = [&](int kt, auto ph_tag) {
     constexpr int PH = decltype(ph_tag)::value;
-    const uint64_t src_a = base_a + static_cast<uint64_t>(kt) * g.a_step, src_b = base_b + static_cast<uint64_t>(kt) * kMxPanelStep;
-    if (PH == 0) copy_to_lds_16B(dst_s + ((kt >> 2) & 1) * kMxScales, base_s + static_cast<uint64_t>(kt >> 2) * s_step, s_off);
+    const uint64_t k = min(kt, KR - 1);
+    const uint64_t src_a = base_a + k * g.a_step, src_b = base_b + k * kMxPanelStep;
+    if (PH == 0) copy_to_lds_16B(__builtin_amdgcn_readfirstlane(dst_s + ((kt >> 2) & 1) * kMxScales), base_s + static_cast<uint64_t>(kt >> 2) * s_step, s_off);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      copy_to_lds_16B(dst_a + PH * kMxStage + kMxTile * 64 + i * 1024, src_b + i * 1024, lane16);
-      copy_to_lds_16B(dst_a + PH * kMxStage + i * 1024, src_a, a_off[i]);
+      copy_to_lds_16B(__builtin_amdgcn_readfirstlane(dst_a + PH * kMxStage + kMxTile * 64 + i * 1024), src_b + i * 1024, lane16);
+      copy_to_lds_16B(__builtin_amdgcn_readfirstlane(dst_a + PH * kMxStage + i * 1024), src_a, a_off[i]);
     }
   };
 
@@ -125,20 +129,19 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
     constexpr int H0 = (TMV + 1) / 2, H1 = TMV / 2;
     mx_u32x4 af0[TM], af1[TM], bf[TN];
     uint32_t xs[TM], ws[TN];
+    const uint32_t tail_mask = (KR & 3) ? (1u << (8 * (KR & 3))) - 1u : ~0u;  // A's scales past K are not written
     auto load_scales = [&](int q, uint32_t* x, uint32_t* w) {
       const unsigned char* p = fs + (q & 1) * kMxScales;
+      const uint32_t mask = q == NG - 1 ? tail_mask : ~0u;
 #pragma unroll
-      for (int tm = 0; tm < TMV; ++tm) x[tm] = *reinterpret_cast<const uint32_t*>(p + ((tm * WAVES_M + wm) * 16 + r16) * 16 + kb * 4);
+      for (int tm = 0; tm < TMV; ++tm) x[tm] = *reinterpret_cast<const uint32_t*>(p + ((tm * WAVES_M + wm) * 16 + r16) * 16 + kb * 4) & mask;
 #pragma unroll
       for (int tn = 0; tn < TN; ++tn)
         w[tn] = *reinterpret_cast<const uint32_t*>(p + kMxTile * 16 + (wn * (EPI == EPI_H ? 2 : 4) + b_sub(tn)) * 256 + lane * 4);
     };
-    auto wait_barrier = [&](int vm) {
+    auto wait_barrier = [&](auto vm_tag) {
       asm volatile("" ::: "memory");
-      if (vm == 9) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(9));
-      else if (vm == 8) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(8));
-      else if (vm == 4) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(4));
-      else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(decltype(vm_tag)::value));
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
@@ -146,12 +149,15 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
     // does not have yet is read while the one before multiplies: phase 0 reads the second half's activations, phase 1, after
     // the barrier that publishes the next step, that step's first half and weights.  The wavefronts that share a SIMD (w and
     // w + 4) issue their copies at different ends of the step, so that one's run under the other's MFMAs.
-    auto step = [&](int kt, auto ph_tag) {
-      constexpr int PH = decltype(ph_tag)::value;
+    // left_tag: steps from this one to the last, as far as they matter here (8: enough).
+    auto step = [&](int kt, auto ph_tag, auto left_tag) {
+      constexpr int PH = decltype(ph_tag)::value, LEFT = decltype(left_tag)::value;
+      // copies that may still be on their way at the barrier: those of steps kt + 2 and kt + 3, and scales that go with one
+      constexpr int VM = LEFT > 3 ? (PH == 1 || PH == 2 ? 9 : 8) : LEFT > 2 ? (PH == 2 ? 5 : 4) : 0;
       constexpr int NX = (PH + 1) & 3;
       const unsigned char* pa = fa + (PH >= 2 ? 2 * kMxStage : 0) + (PH & 1) * kMxStage;
       const unsigned char *na = fa + (NX >= 2 ? 2 * kMxStage : 0) + (NX & 1) * kMxStage, *nb = fb + (NX >= 2 ? 2 * kMxStage : 0) + (NX & 1) * kMxStage;
-      if (EARLY && kt + 3 < KT) copy(kt + 3, std::integral_constant<int, (PH + 3) & 3>{});
+      if (EARLY && LEFT > 3) copy(kt + 3, std::integral_constant<int, (PH + 3) & 3>{});
       __builtin_amdgcn_sched_barrier(0);
       if (TMV > 0) {
 #pragma unroll
@@ -168,46 +174,46 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
         __builtin_amdgcn_sched_group_barrier(0x008, H0 * TN - H1, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
-      // copies that may still be on their way: those of steps kt + 2 and kt + 3, and scales that go with one of them
-      wait_barrier(kt + 3 < KT ? (PH == 1 || PH == 2 ? 9 : 8) : kt + 2 < KT ? 4 : 0);
-      if (!EARLY && kt + 4 < KT) copy(kt + 4, ph_tag);
+      if (LEFT > 1) {
+        wait_barrier(std::integral_constant<int, VM>{});
+        if (!EARLY && LEFT > 4) copy(kt + 4, ph_tag);
+      }
       __builtin_amdgcn_sched_barrier(0);
-      if (TMV > 0) {  // behind the last step there is nothing to read but an old stage, for nobody
+      if (TMV > 0) {
 #pragma unroll
         for (int tn = 0; tn < TN; ++tn) {
 #pragma unroll
           for (int i = 0; i < H1; ++i) {
             const int tm = (tn & 1) ? H1 - 1 - i : i;
             acc[H0 + tm][tn] = mx_mfma<PH, PH>(bf[tn], af1[tm], acc[H0 + tm][tn], ws[tn], xs[H0 + tm]);
-            if (tn == 0) af0[i] = frag(na + i * A_STEP);
+            if (LEFT > 1 && tn == 0) af0[i] = frag(na + i * A_STEP);
           }
-          if (tn == 0 && H0 > H1) af0[H0 - 1] = frag(na + (H0 - 1) * A_STEP);
-          bf[tn] = frag(nb + b_sub(tn) * 1024);
+          if (LEFT > 1 && tn == 0 && H0 > H1) af0[H0 - 1] = frag(na + (H0 - 1) * A_STEP);
+          if (LEFT > 1) bf[tn] = frag(nb + b_sub(tn) * 1024);
         }
+        if (LEFT > 1) {
 #pragma unroll
-        for (int i = 0; i < H1; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        }
-        if (H0 > H1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          for (int i = 0; i < H1; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          }
+          if (H0 > H1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
-        for (int i = 1; i < TN; ++i) {
+          for (int i = 1; i < TN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (H1 > 0) __builtin_amdgcn_sched_group_barrier(0x008, H1, 0);
+          }
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          if (H1 > 0) __builtin_amdgcn_sched_group_barrier(0x008, H1, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        if (PH == 3) {
-          __builtin_amdgcn_sched_barrier(0);
-          load_scales((kt + 1) >> 2, xs, ws);
+          if (PH == 3) {
+            __builtin_amdgcn_sched_barrier(0);
+            load_scales((kt + 1) >> 2, xs, ws);
+          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    using P0 = std::integral_constant<int, 0>;
-    using P1 = std::integral_constant<int, 1>;
-    using P2 = std::integral_constant<int, 2>;
     using P3 = std::integral_constant<int, 3>;
-    if (!EARLY && KT > 3) copy(3, P3{});
+    if (!EARLY) copy(3, P3{});
     if (TMV > 0) {
       load_scales(0, xs, ws);
 #pragma unroll
@@ -215,16 +221,16 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
 #pragma unroll
       for (int tn = 0; tn < TN; ++tn) bf[tn] = frag(fb + b_sub(tn) * 1024);
     }
+    using Enough = std::integral_constant<int, 8>;
     int kt = 0;
-    for (; kt + 4 <= KT; kt += 4) {
-      step(kt, P0{});
-      step(kt + 1, P1{});
-      step(kt + 2, P2{});
-      step(kt + 3, P3{});
-    }
-    if (kt < KT) step(kt, P0{});
-    if (kt + 1 < KT) step(kt + 1, P1{});
-    if (kt + 2 < KT) step(kt + 2, P2{});
+    for (; kt + 8 <= KT; kt += 4) mx_for(std::make_integer_sequence<int, 4>{}, [&](auto i) { step(kt + i.value, i, Enough{}); });
+    mx_for(std::make_integer_sequence<int, 4>{}, [&](auto i) { step(kt + i.value, i, std::integral_constant<int, 4 - decltype(i)::value>{}); });
+    // The sums are made here: without this the last products move down to the stores, under their conditions, and what they
+    // are made of spills.
+#pragma unroll
+    for (int tm = 0; tm < TMV; ++tm)
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) asm volatile("" : "+v"(acc[tm][tn]));
 
     // a lane holds eight consecutive output columns of activation row l % 16
 #pragma unroll
@@ -253,12 +259,10 @@ __global__ __launch_bounds__(512) void mx_tile_kernel(MxArgs a) {
   using Q1 = std::integral_constant<int, 1>;
   using Q2 = std::integral_constant<int, 2>;
   copy(0, Q0{});
-  if (KT > 1) copy(1, Q1{});
-  if (KT > 2) copy(2, Q2{});
+  copy(1, Q1{});
+  copy(2, Q2{});
   asm volatile("" ::: "memory");
-  if (KT > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(8));
-  else if (KT > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(4));
-  else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(8));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   auto pick = [&](auto early) {
