@@ -119,7 +119,7 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
     off = w.off_h;
     auto codes_and_scales = [&off](int64_t rows, int K, size_t& codes, size_t& scales) {
       codes = off;
-      off = align_up(off + static_cast<size_t>(rows) * mx_steps(K) * (kMxStep / 2), 256);
+      off = align_up(off + static_cast<size_t>(rows) * mx_code_row(K), 256);
       scales = off;
       off = align_up(off + static_cast<size_t>(rows) * mx_scale_row(K), 256);
     };

@@ -69,8 +69,8 @@ struct Workspace {
   size_t off_h;           // dtype [N_max * I]
   size_t off_h_shared;    // dtype [T_max * I_shared]
   // the 4-bit FFN's, over off_h and off_h_shared: a context runs one FFN at a time
-  size_t off_mx_x, off_mx_x_scales;                // x: codes [T_max][steps of H][64], scales [T_max][mx_scale_row(H)]
-  size_t off_mx_h, off_mx_h_scales;                // h: codes [steps of I][N_max][64], scales [N_max][mx_scale_row(I)]
+  size_t off_mx_x, off_mx_x_scales;                // x: codes [T_max][mx_code_row(H)], scales [T_max][mx_scale_row(H)]
+  size_t off_mx_h, off_mx_h_scales;                // h: codes (mx_h_at), scales [N_max][mx_scale_row(I)]
   size_t off_mx_h_shared, off_mx_h_shared_scales;  // the shared expert's h
   size_t bytes;
 };

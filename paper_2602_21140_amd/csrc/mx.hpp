@@ -35,6 +35,9 @@ inline int64_t mx_packed_bytes(int rows, int K) { return mx_packed_codes(rows, K
 // lane's results of both blocks are eight consecutive rows of the matrix, i.e. output columns: a word of codes, 16 bytes of bf16.
 __host__ __device__ inline int mx_row(int s, int m) { return 8 * (m >> 2) + 4 * s + (m & 3); }
 
+// Bytes of a row's codes where the kernels keep activations: whole pairs of steps, whole lines.
+__host__ __device__ inline int64_t mx_code_row(int K) { return static_cast<int64_t>((mx_steps(K) + 1) / 2) * kMxStep; }
+
 // Bytes of a row's scales where the kernels keep activations: [groups][4 blocks of a step][4 steps].
 __host__ __device__ inline int mx_scale_row(int K) { return mx_groups(K) * (kMxGroup / kMxBlock); }
 __host__ __device__ inline int mx_scale_at(int block) { return (block & ~15) + ((block & 3) << 2) + ((block >> 2) & 3); }

@@ -32,14 +32,14 @@ MxProblem mx_problem(const revive_ctx* ctx, const MxFfn& f, bool shared, int til
   p.b_codes = mx_packed_codes(p.n_out, p.K);
   if (EPI == EPI_H) {
     p.A = ctx->d_ws + w.off_mx_x;
-    p.a_row = mx_steps(c.H) * (kMxStep / 2); p.a_step = kMxStep / 2;
+    p.a_row = mx_code_row(c.H); p.a_pair = kMxStep;
     p.A_scales = ctx->d_ws + w.off_mx_x_scales;
     p.src_of = shared ? nullptr : f.src_of; p.k = c.k;
     p.b_half = mx_packed_bytes(I, c.H);
     p.H = h; p.H_scales = h_scales; p.h_rows = rows;
   } else {
     p.A = h;
-    p.a_row = kMxStep / 2; p.a_step = static_cast<int64_t>(rows) * (kMxStep / 2);
+    p.a_row = kMxStep; p.a_pair = static_cast<int64_t>(rows) * kMxStep;
     p.A_scales = h_scales;
     p.Y = static_cast<uint16_t*>(shared ? f.y_shared : f.y_perm);
   }
@@ -96,7 +96,7 @@ int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
   if (rc != REVIVE_OK) return rc;
   const MxFfn f{src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * c.k, y_shared ? T : 0};
   // The tiles address a row of x by 32 bits.
-  if (f.N > 64 * ctx->P && static_cast<int64_t>(T) * mx_steps(c.H) * (kMxStep / 2) < (1ll << 32)) return mx_tile_ffn(ctx, f, stream);
+  if (f.N > 64 * ctx->P && static_cast<int64_t>(T) * mx_code_row(c.H) < (1ll << 32)) return mx_tile_ffn(ctx, f, stream);
   return mx_stream_ffn<4, 4, 4>(ctx, f, stream);
 }
 

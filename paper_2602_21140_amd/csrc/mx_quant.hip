@@ -200,7 +200,7 @@ int launch_mx_quantize_tiled(revive_ctx* ctx, const void* x, int64_t rows, int K
   QuantArgs a{};
   a.x = x; a.rows = rows; a.ld = K; a.K = K;
   a.units = mx_steps(K) * (kMxStep / 8);
-  a.codes = codes; a.code_row = mx_steps(K) * (kMxStep / 2);
+  a.codes = codes; a.code_row = mx_code_row(K);
   a.scales = scales; a.scale_row = mx_scale_row(K);
   KernelTimer timer(ctx, REVIVE_K_MX_QUANTIZE, stream);
   return launch_quantize<uint16_t, true>(a, stream, ctx);

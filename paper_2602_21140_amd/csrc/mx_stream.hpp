@@ -23,9 +23,12 @@ namespace revive {
 
 enum { EPI_H = 0, EPI_Y = 1 };
 
+// h, the activations of the second product: [pairs of steps][rows][128 bytes]; where the 64 bytes of step s of a row begin.
+__host__ __device__ inline int64_t mx_h_at(int s, int64_t rows, int64_t row) { return (static_cast<int64_t>(s >> 1) * rows + row) * 128 + (s & 1) * 64; }
+
 struct MxProblem {
-  const uint8_t* A;          // codes of row r, step s: A + r * a_row + s * a_step, 64 bytes
-  int64_t a_row, a_step;
+  const uint8_t* A;          // codes of row r, step s: A + r * a_row + s / 2 * a_pair + s % 2 * 64, 64 bytes
+  int64_t a_row, a_pair;
   const uint8_t* A_scales;   // rows of mx_scale_row(K) bytes
   const int32_t* src_of;     // not null: row r of the product is row src_of[r] / k of A
   int k;
@@ -33,7 +36,7 @@ struct MxProblem {
   const void* B_one;         // the one packed matrix (dense)
   int64_t b_half;            // EPI_H: bytes from the gate matrix to the up matrix
   int64_t b_codes;           // bytes from a matrix' codes to its scales
-  uint8_t* H; uint8_t* H_scales;  // EPI_H: codes [panel of 128 columns][h_rows][64 bytes], scales [h_rows][mx_scale_row(n_out)]
+  uint8_t* H; uint8_t* H_scales;  // EPI_H: codes at mx_h_at, scales [h_rows][mx_scale_row(n_out)]
   int64_t h_rows;
   uint16_t* Y;               // EPI_Y: bf16 [rows, n_out]
   int n_out, K;
@@ -155,7 +158,10 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     uint32_t ws[W], xs[TM], ws_next[W], xs_next[TM];
     auto load_a = [&](int q) {
 #pragma unroll
-      for (int i = 0; i < NA; ++i) af[i] = mx_load16(a_src[i] + min(q * 4 + a_part[i], KT - 1) * g.a_step);
+      for (int i = 0; i < NA; ++i) {
+        const int s = min(q * 4 + a_part[i], KT - 1);
+        af[i] = mx_load16(a_src[i] + (s >> 1) * g.a_pair + (s & 1) * 64);
+      }
     };
     auto load_scales = [&](int q, uint32_t* w, uint32_t* x) {
 #pragma unroll
@@ -224,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
           uint32_t byte;
           const uint32_t codes = mx_swiglu_codes(acc[2 * p][i], acc[2 * p + 1][i], acc[W / 2 + 2 * p][i], acc[W / 2 + 2 * p + 1][i], byte);
           if (row >= row_end || set >= n_sets) continue;
-          *reinterpret_cast<uint32_t*>(g.H + (static_cast<int64_t>(set >> 2) * g.h_rows + row) * 64 + (set & 3) * 16 + kb * 4) = codes;
+          *reinterpret_cast<uint32_t*>(g.H + mx_h_at(set >> 2, g.h_rows, row) + (set & 3) * 16 + kb * 4) = codes;
           if (kb == 0) g.H_scales[static_cast<int64_t>(row) * mx_scale_row(g.n_out) + mx_scale_at(set)] = static_cast<uint8_t>(byte);
         } else {
           const int col = set * 32 + kb * 8;
