@@ -251,10 +251,10 @@ int revive_route(revive_ctx* ctx, const void* x, const void* w_router, float* lo
  *   n_group > 1: a group scores the sum of its two best keys above -inf, in fp32.
  *   topk_weight: the chosen expert's score (without the bias); renormalise != 0:
  *              over the sum of the chosen scores; then times route_scale.
- * A NaN key orders nothing: its expert counts as absent while live experts with
- * numbers are left, in its group's score too, and is chosen after them in
- * ascending id (its weight is NaN; renormalised, so are its row's).  Bias may be
- * infinite: -inf puts an expert behind all others, +inf in front of them.
+ * A key that is NaN or -inf orders nothing: its expert counts as absent while
+ * live experts with other keys are left, in its group's score too, and is chosen
+ * after them, in ascending id (the weight of a NaN score is NaN; renormalised, so
+ * are its row's).  Bias may be infinite: +inf puts an expert in front of all others.
  * Everything else (mask, ties, replicas, token offset) is revive_route's. */
 int revive_route_biased(revive_ctx* ctx, const void* x, const void* w_router, float* logits,
                         int32_t logits_given, const float* bias, int32_t renormalise, int32_t T,

@@ -5,8 +5,8 @@
 //   a group's score is the sum of its two best keys above -inf (the one, if there is one); the topk_group best groups are kept
 //   top-k by key, ties to the lower id;  weight_j = s_{e_j} [/ sum_j s_{e_j}] * route_scale
 //
-// All of it in fp32.  The keys are compared as integers whose order is that of the numbers, which gives what is no number a
-// place: 0 = taken or in a dropped group, 1 = no live replica, 2 = NaN, from 3 on the numbers.
+// All of it in fp32.  What is no number has a place among the keys: NaN and -inf are kNone or less, behind every number and alike
+// but for their ids; an expert that is lost, taken or in a dropped group is -inf.
 #include "ctx.hpp"
 
 namespace revive {
@@ -26,16 +26,18 @@ struct BiasedParams {
   float route_scale;
 };
 
-constexpr uint32_t kTaken = 0, kLost = 1, kNaN = 2, kLowest = 0x007FFFFF;
+constexpr float kNone = -1e38f;
+constexpr float kOut = -__builtin_inff();
 
-// Order-preserving integer of a number: -inf is the lowest, kLowest.
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t b = __float_as_uint(v);
-  return v != v ? kNaN : b ^ (static_cast<uint32_t>(static_cast<int>(b) >> 31) | 0x80000000u);
+// Bias of an expert, made so that the sum with a score (kNone if it is NaN) is the key.
+__device__ __forceinline__ float bias_of(const BiasedParams& p, int e, bool is) {
+  e = min(e, p.E - 1);
+  const float b = p.bias[e];
+  const int count = p.l2p_count[e];
+  return is && count > 0 ? fmaxf(b, kNone) : kOut;
 }
-__device__ __forceinline__ float number(uint32_t u) {  // of a key from 3 on
-  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-}
+// Score of a group from its two best keys.
+__device__ __forceinline__ float group_score(float m1, float m2) { return m2 < 0.5f * kNone ? m1 : m1 + m2; }
 
 // Cross-lane steps as operands of an ALU instruction: 0 to 3 combine lanes 1, 2, 4 and 8 apart inside rows of 16, after which
 // every lane of a row has the row's result; 4 and 5 bring the rows' results to lanes 31 and 63, and then to lane 63; 6 and 7
@@ -47,16 +49,8 @@ __device__ __forceinline__ int dpp(int v, int other) {
   return __builtin_amdgcn_update_dpp(other, v, ctrl, rows, 0xF, false);
 }
 template <int STEP>
-__device__ __forceinline__ uint32_t dpp_u(uint32_t v) { return static_cast<uint32_t>(dpp<STEP>(static_cast<int>(v), 0)); }
-template <int STEP>
 __device__ __forceinline__ float dpp_f(float v, float other) { return __int_as_float(dpp<STEP>(__float_as_int(v), __float_as_int(other))); }
 
-__device__ __forceinline__ uint32_t row_max(uint32_t v) {
-  v = max(v, dpp_u<0>(v));
-  v = max(v, dpp_u<1>(v));
-  v = max(v, dpp_u<2>(v));
-  return max(v, dpp_u<3>(v));
-}
 __device__ __forceinline__ int row_min(int v) {
   v = min(v, dpp<0>(v, 0));
   v = min(v, dpp<1>(v, 0));
@@ -76,16 +70,10 @@ __device__ __forceinline__ float row_sum(float v) {  // by exchanges, so that ev
   return v + dpp_f<7>(v, 0.f);
 }
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  v = row_max(v);
-  v = max(v, dpp_u<4>(v));
-  return static_cast<uint32_t>(last_lane(static_cast<int>(max(v, dpp_u<5>(v)))));
-}
 __device__ __forceinline__ float wave_max(float v) {
-  const float NEG = -__builtin_inff();
   v = row_max(v);
-  v = fmaxf(v, dpp_f<4>(v, NEG));
-  return __int_as_float(last_lane(__float_as_int(fmaxf(v, dpp_f<5>(v, NEG)))));
+  v = fmaxf(v, dpp_f<4>(v, kOut));
+  return __int_as_float(last_lane(__float_as_int(fmaxf(v, dpp_f<5>(v, kOut)))));
 }
 __device__ __forceinline__ float wave_sum(float v) {
   v = row_sum(v);
@@ -94,22 +82,24 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 // The two largest of two disjoint sets, each given by its two largest.
 template <int STEP>
-__device__ __forceinline__ void top2_step(uint32_t& m1, uint32_t& m2) {
-  const uint32_t o1 = dpp_u<STEP>(m1), o2 = dpp_u<STEP>(m2);
-  m2 = max(min(m1, o1), max(m2, o2));
-  m1 = max(m1, o1);
+__device__ __forceinline__ void top2_step(float& m1, float& m2) {
+  const float o1 = dpp_f<STEP>(m1, kOut), o2 = dpp_f<STEP>(m2, kOut);
+  m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+  m1 = fmaxf(m1, o1);
 }
 
-// exp(x) for x in [-100, 88]: 2^p with p = x log2(e) rounded, times what the rounding left out.  Off by two units in the last
-// place; __expf, which lacks the second factor, by as many as |x| says.  NaN stays.
+// The keys' scores.  exp by the hardware's 2^p with p = x log2(e) rounded is off by |x| units in its last place, which is less
+// than one of the largest score; NaN stays, and infinities give what they should.
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ float near_exp(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
+__device__ __forceinline__ float near_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2e)); }
+// The weights' scores, of the chosen experts: exp(x) for x in [-100, 88] with what the rounding of p left out.
 __device__ __forceinline__ float exp_of(float x) {
-  constexpr float kLog2e = 1.44269504f;
   const float p = x * kLog2e, rest = fmaf(x, kLog2e, -p) + x * 1.92596299e-8f;  // log2(e) = kLog2e + 1.92596299e-8
   const float e = __builtin_amdgcn_exp2f(p);
   return fmaf(e, rest * 0.693147181f, e);
 }
-// Softmax: the numerator, m the largest logit.  exp(-100) is zero in fp32.
-__device__ __forceinline__ float exp_below(float z, float m) {
+__device__ __forceinline__ float exp_below(float z, float m) {  // exp(-100) is zero in fp32
   const float d = z - m;
   return exp_of(d < -100.f ? -100.f : d);
 }
@@ -139,116 +129,116 @@ __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j
 template <int V, bool GROUPED, bool WIDE>
 __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, int rounds) {
   constexpr int C = V / 4;
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   typedef float f32x4 __attribute__((ext_vector_type(4)));
-  __shared__ u32x4 keys[4][C][64];
+  __shared__ f32x4 keys[4][C][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane >> 4, li = lane & 15;
-  const float NEG = -__builtin_inff();
   const int n = (p.E + 15) >> 4;
   const int lg = GROUPED ? 16 / p.n_group : 16, lj = li & (lg - 1);  // lanes of a group, this one's place among them
   const int e0 = GROUPED ? li / lg * (p.E / p.n_group) : 0;          // the group's first expert
   auto expert = [&](int i) { return e0 + (WIDE ? (i >> 2) * 4 * lg + lj * 4 + (i & 3) : i * lg + lj); };  // place i
   const bool sig = p.score_fn == REVIVE_SCORE_SIGMOID;
   float bias[V];
-  bool live[V], is[V];  // is: there is an expert in this place
+  if (WIDE) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    is[i] = i < n && expert(i) < p.E;
-    const int e = min(expert(i), p.E - 1);
-    bias[i] = p.bias[e];
-    live[i] = p.l2p_count[e] > 0;
+    for (int c = 0; c < C; ++c) {
+      const int e = c * 4 < n ? expert(c * 4) : 0;  // n is a multiple of 4
+      const f32x4 b = *reinterpret_cast<const f32x4*>(p.bias + e);
+      const int4 k = *reinterpret_cast<const int4*>(p.l2p_count + e);
+      bias[c * 4] = c * 4 < n && k.x > 0 ? fmaxf(b[0], kNone) : kOut;
+      bias[c * 4 + 1] = c * 4 < n && k.y > 0 ? fmaxf(b[1], kNone) : kOut;
+      bias[c * 4 + 2] = c * 4 < n && k.z > 0 ? fmaxf(b[2], kNone) : kOut;
+      bias[c * 4 + 3] = c * 4 < n && k.w > 0 ? fmaxf(b[3], kNone) : kOut;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) bias[i] = bias_of(p, expert(i), i < n && expert(i) < p.E);
   }
   for (int r = 0; r < rounds; ++r) {
     const int t0 = ((r * gridDim.x + blockIdx.x) * 4 + wave) * 4, t = t0 + row;
     if (t0 >= p.T) return;  // whole wavefront leaves together
     const float* z = p.logits + static_cast<int64_t>(min(t, p.T - 1)) * p.E;
-    float s[V];  // logits, then scores
+    f32x4 s[C];  // logits, then scores, then keys
 #pragma unroll
-    for (int i = 0; i < V; i += WIDE ? 4 : 1) {
+    for (int c = 0; c < C; ++c) {
       if (WIDE) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(z + (i < n ? expert(i) : 0));  // n is a multiple of 4
-        s[i] = v[0]; s[i + 1] = v[1]; s[i + 2] = v[2]; s[i + 3] = v[3];
+        s[c] = *reinterpret_cast<const f32x4*>(z + (c * 4 < n ? expert(c * 4) : 0));
+        if (c * 4 >= n) s[c] = f32x4{kOut, kOut, kOut, kOut};  // no experts in these places: scores of zero
       } else {
-        s[i] = z[min(expert(i), p.E - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[c][i] = z[min(expert(c * 4 + i), p.E - 1)];
+          if (c * 4 + i >= n || expert(c * 4 + i) >= p.E) s[c][i] = kOut;
+        }
       }
     }
-    float shift = 0.f, scale = 1.f;
+    float shift = kOut, scale = 1.f;
     if (sig) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = sigmoid(s[i]);
+      for (int i = 0; i < V; ++i) s[i >> 2][i & 3] = near_sigmoid(s[i >> 2][i & 3]);
     } else {
-      shift = NEG;
 #pragma unroll
-      for (int i = 0; i < V; ++i) shift = is[i] ? fmaxf(shift, s[i]) : shift;
+      for (int i = 0; i < V; ++i) shift = fmaxf(shift, s[i >> 2][i & 3]);
       shift = row_max(shift);
       float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        s[i] = exp_below(s[i], shift);
-        sum += is[i] ? s[i] : 0.f;
-      }
+      for (int i = 0; i < V; ++i) sum += s[i >> 2][i & 3] = near_exp(s[i >> 2][i & 3], shift);
       scale = 1.0f / row_sum(sum);
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] *= scale;
+      for (int i = 0; i < V; ++i) s[i >> 2][i & 3] *= scale;
     }
-    uint32_t best4[C];
-    u32x4 u[C];
 #pragma unroll
-    for (int i = 0; i < V; ++i) u[i >> 2][i & 3] = !is[i] ? kTaken : live[i] ? ordered(s[i] + bias[i]) : kLost;
+    for (int i = 0; i < V; ++i) s[i >> 2][i & 3] = fmaxf(s[i >> 2][i & 3], kNone) + bias[i];
     if (GROUPED) {
-      uint32_t m1 = 0, m2 = 0;
+      float m1 = kOut, m2 = kOut;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        m2 = max(min(m1, u[i >> 2][i & 3]), m2);
-        m1 = max(m1, u[i >> 2][i & 3]);
+        m2 = fmaxf(fminf(m1, s[i >> 2][i & 3]), m2);
+        m1 = fmaxf(m1, s[i >> 2][i & 3]);
       }
       top2_step<0>(m1, m2);
       if (lg >= 4) top2_step<1>(m1, m2);
       if (lg >= 8) top2_step<6>(m1, m2);
-      const float g = m1 <= kLowest ? NEG : m2 <= kLowest ? number(m1) : number(m1) + number(m2);
       // rank of my group among all groups of the token (better score first, ties to the lower group id)
-      const uint32_t mine = ordered(g);
-      int rank = 0;
-      uint32_t o = mine;
-      int h = li;
+      const float mine = group_score(m1, m2);
+      int rank = 0, o = __float_as_int(mine), h = li;
       for (int i = 1; i < p.n_group; ++i) {  // rotate the row by a group
-        if (lg == 2) { o = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(o), 0x122, 0xF, 0xF, false)); h = __builtin_amdgcn_mov_dpp(h, 0x122, 0xF, 0xF, false); }
-        else if (lg == 4) { o = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(o), 0x124, 0xF, 0xF, false)); h = __builtin_amdgcn_mov_dpp(h, 0x124, 0xF, 0xF, false); }
-        else { o = static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(o), 0x128, 0xF, 0xF, false)); h = __builtin_amdgcn_mov_dpp(h, 0x128, 0xF, 0xF, false); }
-        rank += o > mine || (o == mine && h < li);
+        if (lg == 2) { o = __builtin_amdgcn_mov_dpp(o, 0x122, 0xF, 0xF, false); h = __builtin_amdgcn_mov_dpp(h, 0x122, 0xF, 0xF, false); }
+        else if (lg == 4) { o = __builtin_amdgcn_mov_dpp(o, 0x124, 0xF, 0xF, false); h = __builtin_amdgcn_mov_dpp(h, 0x124, 0xF, 0xF, false); }
+        else { o = __builtin_amdgcn_mov_dpp(o, 0x128, 0xF, 0xF, false); h = __builtin_amdgcn_mov_dpp(h, 0x128, 0xF, 0xF, false); }
+        rank += __int_as_float(o) > mine || (__int_as_float(o) == mine && h < li);
       }
       const bool kept = rank < p.topk_group;
 #pragma unroll
-      for (int i = 0; i < V; ++i) u[i >> 2][i & 3] = kept ? u[i >> 2][i & 3] : kTaken;
+      for (int i = 0; i < V; ++i) s[i >> 2][i & 3] = kept ? s[i >> 2][i & 3] : kOut;
     }
+    float best4[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      best4[c] = max(max(u[c][0], u[c][1]), max(u[c][2], u[c][3]));
-      if (C > 1) keys[wave][c][lane] = u[c];
+      best4[c] = fmaxf(fmaxf(s[c][0], s[c][1]), fmaxf(s[c][2], s[c][3]));
+      if (C > 1) keys[wave][c][lane] = s[c];
     }
-    __builtin_amdgcn_wave_barrier();
 
     // k rounds of arg-max (largest key, ties to the lower expert id); lane j of the row keeps the j-th choice
-    constexpr int kNone = 1 << 16;
+    constexpr int kNobody = 1 << 16;
     int my_e = 0;
 #pragma unroll 1
     for (int j = 0; j < p.k; ++j) {
-      uint32_t m = best4[0];
+      float m = best4[0];
 #pragma unroll
-      for (int c = 1; c < C; ++c) m = max(m, best4[c]);
-      const uint32_t best = row_max(m);
+      for (int c = 1; c < C; ++c) m = fmaxf(m, best4[c]);
+      const float best = row_max(m);
       int at = C - 1;
 #pragma unroll
       for (int c = C - 2; c >= 0; --c) at = best4[c] == best ? c : at;
-      u32x4 four = C > 1 ? keys[wave][at][lane] : u[0];
+      f32x4 four = C > 1 ? keys[wave][at][lane] : s[0];
       const int pos = four[0] == best ? 0 : four[1] == best ? 1 : four[2] == best ? 2 : 3;
-      const int mine = m == best ? expert(at * 4 + pos) : kNone, e = row_min(mine);
+      const int mine = m == best ? expert(at * 4 + pos) : kNobody, e = row_min(mine);
       const bool won = mine == e;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) four[i] = won && pos == i ? kTaken : four[i];
+      for (int i = 0; i < 4; ++i) four[i] = won && pos == i ? kOut : four[i];
       if (C > 1) keys[wave][at][lane] = four;
-      else u[0] = four;
-      const uint32_t left = max(max(four[0], four[1]), max(four[2], four[3]));
+      else s[0] = four;
+      const float left = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
 #pragma unroll
       for (int c = 0; c < C; ++c) best4[c] = won && at == c ? left : best4[c];
       my_e = li == j ? e : my_e;
@@ -267,81 +257,100 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   const int lane = threadIdx.x & 63;
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= p.T) return;  // whole wavefront leaves together
-  const float NEG = -__builtin_inff();
-  float score[V];
-  uint32_t key[V];
-  float m = NEG;
+  const float* z = p.logits + static_cast<int64_t>(t) * p.E;
+  const bool sig = p.score_fn == REVIVE_SCORE_SIGMOID;
+  float key[V], bias[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int e = lane + 64 * i;
-    score[i] = e < p.E ? p.logits[static_cast<int64_t>(t) * p.E + e] : NEG;
-    m = fmaxf(m, score[i]);
+    key[i] = e < p.E ? z[e] : kOut;
+    bias[i] = bias_of(p, e, e < p.E);
   }
-  if (p.score_fn == REVIVE_SCORE_SIGMOID) {
+  float shift = kOut, scale = 1.f;
+  if (sig) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) score[i] = sigmoid(score[i]);
+    for (int i = 0; i < V; ++i) key[i] = near_sigmoid(key[i]);
   } else {
-    m = wave_max(m);
+#pragma unroll
+    for (int i = 0; i < V; ++i) shift = fmaxf(shift, key[i]);
+    shift = wave_max(shift);
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      score[i] = lane + 64 * i < p.E ? exp_below(score[i], m) : 0.f;
-      sum += score[i];
-    }
-    sum = wave_sum(sum);
+    for (int i = 0; i < V; ++i) sum += key[i] = near_exp(key[i], shift);
+    scale = 1.0f / wave_sum(sum);
 #pragma unroll
-    for (int i = 0; i < V; ++i) score[i] /= sum;
+    for (int i = 0; i < V; ++i) key[i] *= scale;
   }
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = lane + 64 * i;
-    key[i] = e >= p.E ? kTaken : p.l2p_count[e] > 0 ? ordered(score[i] + p.bias[e]) : kLost;
-  }
+  for (int i = 0; i < V; ++i) key[i] = fmaxf(key[i], kNone) + bias[i];
 
   if (p.n_group > 1) {
     const int gsz = p.E / p.n_group;
-    float mine = NEG;  // score of group `lane`
-    for (int g = 0; g < p.n_group; ++g) {
-      uint32_t m1 = 0, m2 = 0;
+    float mine = kOut;  // score of group `lane`
+    if (gsz >= 8 && (gsz & (gsz - 1)) == 0 && gsz <= 64) {  // groups are aligned runs of lanes: all of them at once
+      const int per = 64 / gsz, src = (lane % per) * gsz;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const int e = lane + 64 * i;
-        const uint32_t u = e >= g * gsz && e < (g + 1) * gsz ? key[i] : 0;
-        m2 = max(m2, min(m1, u));
-        m1 = max(m1, u);
+        float m1 = key[i], m2 = kOut;
+        top2_step<0>(m1, m2);
+        top2_step<1>(m1, m2);
+        top2_step<6>(m1, m2);
+        if (gsz >= 16) top2_step<7>(m1, m2);
+        if (gsz >= 32) {
+          const float o1 = __shfl_xor(m1, 16), o2 = __shfl_xor(m2, 16);
+          m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+          m1 = fmaxf(m1, o1);
+        }
+        if (gsz >= 64) {
+          const float o1 = __shfl_xor(m1, 32), o2 = __shfl_xor(m2, 32);
+          m2 = fmaxf(fminf(m1, o1), fmaxf(m2, o2));
+          m1 = fmaxf(m1, o1);
+        }
+        const float g = __shfl(group_score(m1, m2), src);
+        if (lane / per == i && lane < p.n_group) mine = g;
       }
-      top2_step<0>(m1, m2);
-      top2_step<1>(m1, m2);
-      top2_step<6>(m1, m2);
-      top2_step<7>(m1, m2);
-      top2_step<4>(m1, m2);
-      top2_step<5>(m1, m2);
-      m1 = static_cast<uint32_t>(last_lane(static_cast<int>(m1)));
-      m2 = static_cast<uint32_t>(last_lane(static_cast<int>(m2)));
-      const float s = m1 <= kLowest ? NEG : m2 <= kLowest ? number(m1) : number(m1) + number(m2);
-      if (lane == g) mine = s;
+    } else {
+      for (int g = 0; g < p.n_group; ++g) {
+        float m1 = kOut, m2 = kOut;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int e = lane + 64 * i;
+          const float u = e >= g * gsz && e < (g + 1) * gsz ? key[i] : kOut;
+          m2 = fmaxf(m2, fminf(m1, u));
+          m1 = fmaxf(m1, u);
+        }
+        top2_step<0>(m1, m2);
+        top2_step<1>(m1, m2);
+        top2_step<6>(m1, m2);
+        top2_step<7>(m1, m2);
+        top2_step<4>(m1, m2);
+        top2_step<5>(m1, m2);
+        const float s = __int_as_float(last_lane(__float_as_int(group_score(m1, m2))));
+        if (lane == g) mine = s;
+      }
     }
-    const uint32_t mine_u = lane < p.n_group ? ordered(mine) : 0;
     int rank = 0;
     for (int h = 0; h < p.n_group; ++h) {
-      const uint32_t o = static_cast<uint32_t>(__shfl(static_cast<int>(mine_u), h));
-      rank += o > mine_u || (o == mine_u && h < lane);
+      const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), h));
+      rank += o > mine || (o == mine && h < lane);
     }
     const unsigned long long kept = __ballot(lane < p.n_group && rank < p.topk_group);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int g = min((lane + 64 * i) / gsz, 63);
-      if (!((kept >> g) & 1ull)) key[i] = kTaken;
+      // e / gsz: exact, e + 1/2 is never within 2^-11 of a multiple of gsz
+      const int g = static_cast<int>((static_cast<float>(lane + 64 * i) + 0.5f) / static_cast<float>(gsz));
+      if (!((static_cast<uint32_t>(kept) >> (g & 31)) & 1u)) key[i] = kOut;
     }
   }
 
-  int my_e = 0;       // lane j: the j-th choice
-  float my_s = 0.f;
+  // k rounds of arg-max (largest key, ties to the lower expert id); lane j keeps the j-th choice
+  int my_e = 0;
+#pragma unroll 1
   for (int j = 0; j < p.k; ++j) {
-    uint32_t u = 0;
+    float u = key[0];
 #pragma unroll
-    for (int i = 0; i < V; ++i) u = max(u, key[i]);
-    const uint32_t best = wave_max(u);
+    for (int i = 1; i < V; ++i) u = fmaxf(u, key[i]);
+    const float best = wave_max(u);
     int wi = 0;
     unsigned long long holders = 1ull;
 #pragma unroll
@@ -350,21 +359,29 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
       if (b) { holders = b; wi = i; }
     }
     const int w = __builtin_ctzll(holders);
-    float s = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (wi == i) {
-        s = __shfl(score[i], w);
-        if (lane == w) key[i] = kTaken;
-      }
-    if (lane == j) { my_e = min(wi * 64 + w, p.E - 1); my_s = s; }
+      if (wi == i && lane == w) key[i] = kOut;
+    if (lane == j) my_e = min(wi * 64 + w, p.E - 1);
   }
 
-  const float sum = p.renormalise ? wave_sum(lane < p.k ? my_s : 0.f) : 1.f;
-  if (lane < p.k) store_choice(p, t, lane, my_e, my_s / sum * p.route_scale);
+  const float zc = z[my_e];
+  const float sc = sig ? sigmoid(zc) : exp_below(zc, shift) * scale;
+  const float sum = p.renormalise ? wave_sum(lane < p.k ? sc : 0.f) : 1.f;
+  if (lane < p.k) store_choice(p, t, lane, my_e, sc / sum * p.route_scale);
 }
 
 }  // namespace
+
+// Which kernel.  A row of lanes per token does a quarter of the work, but one after the other: it wins once a wavefront per token
+// keeps the ALUs busy, later where experts are no multiple of 64 and its loads are of four bytes.  us in a graph, a row and a
+// wavefront per token: 256 experts in 8 groups, k = 8, 1024 tokens 6.7 and 6.7, 2048 6.8 and 7.4, 8192 7.9 and 14.3; 384, k = 8,
+// 1024 6.5 and 6.2, 2048 6.6 and 6.9, 8192 7.7 and 12.1; 512, k = 16, 1024 10.6 and 9.9, 2048 10.7 and 11.8; 64, k = 2, 2048
+// 3.2 and 2.8, 4096 3.2 and 3.5; 100, k = 4, 4096 5.0 and 4.4, 8192 5.4 and 5.6; 500, k = 8, 4096 12.0 and 10.5, 8192 13.2 and 16.5.
+constexpr int kRowsFrom = 2048, kNarrowRowsFrom = 6144;
+// Workgroups of the rows' kernel at most; beyond them each takes its share of tokens.  32768 tokens, 384 experts: 512 26.7, 1024
+// 21.4, 2048 22.2.
+constexpr int kRowsWorkgroups = 1024;
 
 int launch_route_biased(revive_ctx* ctx, const float* logits, const float* bias, bool renormalise, int T, int32_t* topk_logical,
                         float* topk_weight, int32_t* topk_phys, hipStream_t stream) {
@@ -378,11 +395,12 @@ int launch_route_biased(revive_ctx* ctx, const float* logits, const float* bias,
   p.t_offset = ctx->token_offset; p.route_scale = c.route_scale;
   KernelTimer timer(ctx, REVIVE_K_ROUTE_TOPK, stream);
   const dim3 block(256);
-  const bool rows = c.k <= 16 && (c.n_group == 1 || (c.E % 16 == 0 && (c.n_group == 2 || c.n_group == 4 || c.n_group == 8)));
+  const bool wide = c.E % 64 == 0 && (reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(bias)) % 16 == 0;
+  const bool rows = T >= (wide ? kRowsFrom : kNarrowRowsFrom) && c.k <= 16 &&
+                    (c.n_group == 1 || (c.E % 16 == 0 && (c.n_group == 2 || c.n_group == 4 || c.n_group == 8)));
   if (rows) {
-    const int fours = ceil_div(T, 16), workgroups = fours < 2048 ? fours : 2048, rounds = ceil_div(fours, workgroups);
+    const int fours = ceil_div(T, 16), workgroups = fours < kRowsWorkgroups ? fours : kRowsWorkgroups, rounds = ceil_div(fours, workgroups);
     const int n = ceil_div(c.E, 16);
-    const bool wide = c.E % 64 == 0 && reinterpret_cast<uintptr_t>(logits) % 16 == 0;
 #define REVIVE_ROUTE_LAUNCH(V)                                                                                                             \
   do {                                                                                                                                     \
     if (c.n_group > 1 && wide) hipLaunchKernelGGL((route_biased_rows_kernel<V, true, true>), dim3(workgroups), block, 0, stream, p, rounds);  \

@@ -80,6 +80,31 @@ def test_against_the_oracle(E, n_group, topk_group, k, score_fn, T):
     g.L.close()
 
 
+# many tokens: experts that are no multiple of 64, or of 16, or one more than a form of the kernel holds
+@pytest.mark.parametrize("E,n_group,topk_group,k", [(16, 1, 1, 2), (61, 1, 1, 1), (65, 1, 1, 16), (100, 1, 1, 4), (48, 4, 2, 3), (200, 8, 2, 16),
+                                                    (208, 2, 1, 8), (400, 2, 1, 8), (500, 1, 1, 16), (320, 4, 3, 7), (511, 1, 1, 5)])
+def test_many_tokens(E, n_group, topk_group, k):
+    test_against_the_oracle(E, n_group, topk_group, k, "sigmoid" if k % 2 else "softmax", 6147)
+
+
+def test_more_tokens_than_the_workgroups_take_at_once():
+    test_against_the_oracle(64, 1, 1, 4, "softmax", 33001)
+
+
+def test_logits_and_bias_at_any_address():
+    T, E = 2100, 128
+    g = Gate(E, 4, 2, 6, "sigmoid", T, seed=3)
+    logits, bias = torch.randn(T, E, generator=torch.Generator().manual_seed(1)).cuda(), torch.randn(E, generator=torch.Generator().manual_seed(2)).cuda() / 16
+    want = g.run(logits, bias)
+    for offset in (1, 2, 3):
+        a, b = torch.empty(T * E + 4, device="cuda")[offset:offset + T * E].view(T, E), torch.empty(E + 4, device="cuda")[4 - offset:4 - offset + E]
+        a.copy_(logits), b.copy_(bias)
+        for x, y in ((a, bias), (logits, b), (a, b)):
+            got = g.run(x, y)
+            assert np.array_equal(got[0], want[0]) and np.array_equal(got[2], want[2]) and np.abs(got[1] - want[1]).max() < 1e-6
+    g.L.close()
+
+
 @pytest.mark.parametrize("score_fn", ["softmax", "sigmoid"])
 def test_no_bias_chooses_as_the_gate_without(score_fn):
     g = Gate(256, 8, 4, 8, score_fn, 2000, seed=5)
