@@ -344,7 +344,7 @@ int revive_shared_ffn(revive_ctx* ctx, const void* x, const void* w_sh_gate_up,
  *   scales  dev uint8 [rows, ceil(K/32)]
  * revive_mx_dequantize: the numbers they stand for, [rows, K], fp32 or bf16 (both
  *   hold them exactly), rows ld elements apart.
- * K <= 2^24; rows with a stride and an address of whole 16 bytes are faster. */
+ * K <= 2^24.  Rows may start at any address that fits their elements. */
 int revive_mx_quantize(const void* x, int32_t dtype, int64_t rows, int32_t K, int64_t ld, uint8_t* codes,
                        uint8_t* scales, revive_stream stream);
 int revive_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype,

@@ -255,53 +255,57 @@ def _check_free(rc: int):
         raise ReviveError(rc, lib().revive_last_error(None).decode())
 
 
-def _mx_dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.bfloat16:
-        return DTYPE["bf16"]
-    if t.dtype == torch.float32:
-        return DTYPE["fp32"]
-    raise TypeError(f"microscaled numbers are made of and into float32 and bfloat16, not {t.dtype}")
+_MX_DTYPE = {torch.float32: DTYPE["fp32"], torch.bfloat16: DTYPE["bf16"]}
 
 
-def _mx_form(codes: torch.Tensor, scales: torch.Tensor):
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2:
-        raise ValueError("codes and scales are uint8 matrices")
-    if codes.shape != (scales.shape[0], 16 * scales.shape[1]) or not codes.is_contiguous() or not scales.is_contiguous():
-        raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)}: contiguous [rows, 16 n] and [rows, n] expected")
+def _mx_check_form(codes: torch.Tensor, scales: torch.Tensor, rows: int, n: int):
+    """codes [rows, 16 n] and scales [rows, n], contiguous uint8."""
+    if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or codes.shape != (rows, 16 * n) or scales.shape != (rows, n)
+            or not codes.is_contiguous() or not scales.is_contiguous()):
+        raise ValueError(f"codes {codes.dtype} {tuple(codes.shape)} and scales {scales.dtype} {tuple(scales.shape)}: contiguous uint8 "
+                         f"{(rows, 16 * n)} and {(rows, n)} expected")
 
 
+def _mx_rows(x: torch.Tensor, what: str):
+    """(library dtype, rows, K, elements between rows) of a matrix whose rows are contiguous and do not overlap."""
+    dtype = _MX_DTYPE.get(x.dtype)
+    if dtype is None:
+        raise TypeError(f"{what}: microscaled numbers are made of and into float32 and bfloat16, not {x.dtype}")
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2:
+        raise ValueError(f"{what} is a matrix")
+    rows, K = shape
+    ld = stride[0] if rows > 1 else K
+    if ld < K or (K > 1 and stride[1] != 1):
+        raise ValueError(f"{what} is a matrix whose rows are contiguous and do not overlap")
+    return dtype, rows, K, ld
+
+
+# Both calls' checks are kept short: with a query each for what several of them need, a call took 2 us more.
 def mx_quantize(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """revive_mx_quantize: x [rows, K] fp32 or bf16 (rows may be strided) -> (codes [rows, 16 n], scales [rows, n]), n =
     ceil(K / 32) blocks of 32."""
-    dtype = _mx_dtype(x)
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
-        raise ValueError("x is a matrix whose rows are contiguous and do not overlap")
-    rows, K = x.shape
-    n = -(-K // MX_BLOCK)
+    dtype, rows, K, ld = _mx_rows(x, "x")
+    n = (K + MX_BLOCK - 1) // MX_BLOCK
     if out is None:
         out = (torch.empty(rows, 16 * n, dtype=torch.uint8, device=x.device), torch.empty(rows, n, dtype=torch.uint8, device=x.device))
     codes, scales = out
-    _mx_form(codes, scales)
-    if scales.shape != (rows, n):
-        raise ValueError(f"scales {tuple(scales.shape)}: {(rows, n)} expected")
-    _check_free(lib().revive_mx_quantize(x.data_ptr(), dtype, rows, K, x.stride(0) if rows > 1 else K, codes.data_ptr(),
-                                         scales.data_ptr(), _current_stream(stream)))
+    _mx_check_form(codes, scales, rows, n)
+    _check_free(lib().revive_mx_quantize(x.data_ptr(), dtype, rows, K, ld, codes.data_ptr(), scales.data_ptr(), _current_stream(stream)))
     return codes, scales
 
 
 def mx_dequantize(codes: torch.Tensor, scales: torch.Tensor, K: Optional[int] = None, dtype=torch.bfloat16, out=None,
                   stream=None) -> torch.Tensor:
     """revive_mx_dequantize: the numbers that codes and scales stand for, [rows, K] (default: all of the blocks, or out's)."""
-    _mx_form(codes, scales)
-    rows, n = scales.shape
     if out is None:
+        rows, n = scales.shape
         out = torch.empty(rows, MX_BLOCK * n if K is None else K, dtype=dtype, device=codes.device)
-    if out.dim() != 2 or out.shape[0] != rows or -(-out.shape[1] // MX_BLOCK) != n or (K is not None and out.shape[1] != K):
-        raise ValueError(f"out {tuple(out.shape)} does not fit {rows} rows of {n} blocks")
-    if (out.shape[1] > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < out.shape[1]):
-        raise ValueError("out is a matrix whose rows are contiguous and do not overlap")
-    _check_free(lib().revive_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, out.shape[1], _mx_dtype(out), out.data_ptr(),
-                                           out.stride(0) if rows > 1 else out.shape[1], _current_stream(stream)))
+    code, rows, width, ld = _mx_rows(out, "out")
+    if K is not None and width != K:
+        raise ValueError(f"out {tuple(out.shape)}: {K} columns expected")
+    _mx_check_form(codes, scales, rows, (width + MX_BLOCK - 1) // MX_BLOCK)
+    _check_free(lib().revive_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, width, code, out.data_ptr(), ld, _current_stream(stream)))
     return out
 
 
@@ -313,8 +317,10 @@ def mx_packed_bytes(rows: int, K: int) -> int:
 
 def mx_pack(codes: torch.Tensor, scales: torch.Tensor, out=None, stream=None) -> torch.Tensor:
     """revive_mx_pack: an output-major weight matrix' codes and scales -> uint8 in the order that the 4-bit FFN reads."""
-    _mx_form(codes, scales)
+    if scales.dim() != 2:
+        raise ValueError("codes and scales are matrices")
     rows, K = scales.shape[0], scales.shape[1] * MX_BLOCK
+    _mx_check_form(codes, scales, rows, scales.shape[1])
     n = mx_packed_bytes(rows, K)
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=codes.device)

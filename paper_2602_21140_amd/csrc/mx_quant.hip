@@ -9,9 +9,19 @@ namespace revive {
 
 namespace {
 
-__device__ __forceinline__ uint4 load_16B(const void* p) {
-  const auto v = *reinterpret_cast<const __attribute__((address_space(1))) mx_u32x4*>(reinterpret_cast<uintptr_t>(p));
-  return make_uint4(v[0], v[1], v[2], v[3]);
+// 16 bytes at any address that fits the element: the hardware takes unaligned ones, at the cost of the lines they straddle.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+template <bool ONCE>  // ONCE: past the caches' retention
+__device__ __forceinline__ u32x4 load_16B(const void* p) {
+  const auto q = reinterpret_cast<const __attribute__((address_space(1))) u32x4_any*>(reinterpret_cast<uintptr_t>(p));
+  return ONCE ? __builtin_nontemporal_load(q) : *q;
+}
+template <bool ONCE>
+__device__ __forceinline__ void store_16B(void* p, u32x4 v) {
+  const auto q = reinterpret_cast<__attribute__((address_space(1))) u32x4_any*>(reinterpret_cast<uintptr_t>(p));
+  if (ONCE) __builtin_nontemporal_store(v, q);
+  else *q = v;
 }
 
 // Lanes of four: largest value among them.
@@ -32,10 +42,14 @@ struct QuantArgs {
 };
 
 // A thread takes units of eight numbers, four threads a block: 16 (32) bytes in, four bytes of codes out, so that a wavefront
-// reads and writes in address order.  kUnits of them are in flight.  VEC: rows start on 16 bytes.  TILED: the scales' order is
-// that of the kernels' activations.
+// reads and writes in address order.  kUnits of them are in flight.  TILED: the scales' order is that of the kernels'
+// activations.
+//
+// Bound by HBM.  ONCE (rows larger than the last-level cache): non-temporal loads, here and for the way back non-temporal stores,
+// leave the caches to the codes.
 constexpr int kUnits = 4;
-template <typename El, bool VEC, bool TILED>
+constexpr int64_t kOnceBytes = 256ll << 20;
+template <typename El, bool ONCE, bool TILED>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantArgs a) {
   const int tr = 1 << a.row_threads_log2, col = threadIdx.x & (tr - 1);
   const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> a.row_threads_log2;
@@ -48,11 +62,11 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantArgs a) {
     const int u = u0 + i * tr, k0 = u * 8;
 #pragma unroll
     for (int w = 0; w < static_cast<int>(sizeof(El)) * 2; ++w) raw[i][w] = 0;
-    if (VEC && k0 + 8 <= a.K) {
+    if (k0 + 8 <= a.K) {
 #pragma unroll
       for (int w = 0; w < static_cast<int>(sizeof(El)) / 2; ++w) {
-        const uint4 v = load_16B(x + k0 + w * (16 / sizeof(El)));
-        raw[i][w * 4] = v.x; raw[i][w * 4 + 1] = v.y; raw[i][w * 4 + 2] = v.z; raw[i][w * 4 + 3] = v.w;
+        const u32x4 v = load_16B<ONCE>(x + k0 + w * (16 / sizeof(El)));
+        raw[i][w * 4] = v[0]; raw[i][w * 4 + 1] = v[1]; raw[i][w * 4 + 2] = v[2]; raw[i][w * 4 + 3] = v[3];
       }
     } else {
 #pragma unroll
@@ -90,8 +104,7 @@ int launch_quantize(const QuantArgs& base, hipStream_t stream, const revive_ctx*
   const int64_t gx = (a.rows * (1 << a.row_threads_log2) + 255) / 256;
   if (gx > 0x7fffffff) return fail(ctx, REVIVE_EINVAL, "mx quantize: too many rows");
   const dim3 grid(static_cast<uint32_t>(gx), ceil_div(a.units, kUnits << a.row_threads_log2));
-  const bool vec = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.ld * static_cast<int64_t>(sizeof(El))) % 16 == 0;
-  if (vec) hipLaunchKernelGGL((mx_quantize_kernel<El, true, TILED>), grid, dim3(256), 0, stream, a);
+  if (a.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes) hipLaunchKernelGGL((mx_quantize_kernel<El, true, TILED>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((mx_quantize_kernel<El, false, TILED>), grid, dim3(256), 0, stream, a);
   return check_hip(ctx, hipGetLastError(), "mx_quantize launch");
 }
@@ -103,7 +116,7 @@ struct DequantArgs {
   int K, blocks, units, row_threads_log2;
 };
 
-template <typename El, bool VEC>
+template <typename El, bool ONCE>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantArgs a) {
   const int tr = 1 << a.row_threads_log2, col = threadIdx.x & (tr - 1);
   const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> a.row_threads_log2;
@@ -128,15 +141,15 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantArgs a) {
     uint32_t b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) b[j] = byte[i] == 255u ? 0x7FC00000u : __float_as_uint(p[j / 2][j & 1]);
-    if (VEC && k0 + 8 <= a.K) {
+    if (k0 + 8 <= a.K) {
       if (sizeof(El) == 4) {
-        reinterpret_cast<uint4*>(out + k0)[0] = make_uint4(b[0], b[1], b[2], b[3]);
-        reinterpret_cast<uint4*>(out + k0)[1] = make_uint4(b[4], b[5], b[6], b[7]);
+        store_16B<ONCE>(out + k0, u32x4{b[0], b[1], b[2], b[3]});
+        store_16B<ONCE>(out + k0 + 4, u32x4{b[4], b[5], b[6], b[7]});
       } else {  // two significant bits: bf16 holds every value, subnormal ones too
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = (b[2 * j] >> 16) | (b[2 * j + 1] & 0xFFFF0000u);
-        *reinterpret_cast<uint4*>(out + k0) = make_uint4(w[0], w[1], w[2], w[3]);
+        store_16B<ONCE>(out + k0, u32x4{w[0], w[1], w[2], w[3]});
       }
     } else {
 #pragma unroll
@@ -157,8 +170,7 @@ int launch_dequantize(const DequantArgs& base, hipStream_t stream) {
   const int64_t gx = (a.rows * (1 << a.row_threads_log2) + 255) / 256;
   if (gx > 0x7fffffff) return fail(nullptr, REVIVE_EINVAL, "revive_mx_dequantize: too many rows");
   const dim3 grid(static_cast<uint32_t>(gx), ceil_div(a.units, kUnits << a.row_threads_log2));
-  const bool vec = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && (a.ld * static_cast<int64_t>(sizeof(El))) % 16 == 0;
-  if (vec) hipLaunchKernelGGL((mx_dequantize_kernel<El, true>), grid, dim3(256), 0, stream, a);
+  if (a.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes) hipLaunchKernelGGL((mx_dequantize_kernel<El, true>), grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL((mx_dequantize_kernel<El, false>), grid, dim3(256), 0, stream, a);
   return check_hip(nullptr, hipGetLastError(), "mx_dequantize launch");
 }
@@ -176,9 +188,9 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const uint8_t* __restrict_
     const int steps = mx_steps(K), step = static_cast<int>(rest % steps);
     const int64_t row = row_of(rest / steps, sub, lane);
     const int block = step * 4 + (lane >> 4);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (row < rows && block < blocks) v = load_16B(codes + (row * blocks + block) * 16);
-    reinterpret_cast<uint4*>(packed)[i] = v;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (row < rows && block < blocks) v = load_16B<false>(codes + (row * blocks + block) * 16);
+    reinterpret_cast<u32x4*>(packed)[i] = v;
   } else if (i < n_codes + n_scales) {
     const int64_t o = i - n_codes;
     const int lane = o & 63, sub = (o >> 6) & 7;
