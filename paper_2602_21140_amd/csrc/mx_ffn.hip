@@ -12,6 +12,15 @@ namespace revive {
 
 namespace {
 
+constexpr int kMxCus = 256;
+// Up to so many tokens each workgroup of the first product rounds its rows of x itself.
+constexpr int kMxFewTokens = 16;
+// Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below
+// it the streaming kernel, which starts sooner.  us, streaming and tiles: 288 slots, H = 7168, I = 2048: 14 rows 1146 and 1192,
+// 28 rows 1276 and 1242, 57 rows 1426 and 1329; 72 slots, H = 2048, I = 1408: 21 rows 73 and 75, 43 rows 83 and 82; 40 slots, H =
+// 1024, I = 512: 26 rows 18 and 22, 102 rows 26 and 24; 128 slots, H = 4096, I = 256: 8 rows 57 and 61, 32 rows 79 and 72.
+constexpr int kMxTileRowsPerSlot = 32;
+
 struct MxFfn {
   const int32_t* src_of; const int32_t* slot_offsets; const void* const* w_gate_up; const void* const* w_down; void* y_perm;
   const void* w_sh_gate_up; const void* w_sh_down; void* y_shared;
@@ -64,15 +73,29 @@ MxArgs mx_args(const revive_ctx* ctx, const MxFfn& f, int tile_m, int tile_n) {
   return a;
 }
 
-template <int TMX, int W, int NW>
-int mx_stream_ffn(revive_ctx* ctx, const MxFfn& f, hipStream_t stream) {
-  {
-    KernelTimer timer(ctx, REVIVE_K_MX_GATE_UP, stream);
-    const int rc = launch_mx_stream<TMX, W, NW, EPI_H>(ctx, mx_args<EPI_H>(ctx, f, 16 * TMX, NW * W * 8), stream);
-    if (rc != REVIVE_OK) return rc;
-  }
-  KernelTimer timer(ctx, REVIVE_K_MX_DOWN, stream);
-  return launch_mx_stream<TMX, W, NW, EPI_Y>(ctx, mx_args<EPI_Y>(ctx, f, 16 * TMX, NW * W * 16), stream);
+template <int TMX, int NW, int EPI, bool BF16>
+int mx_stream_as(revive_ctx* ctx, const MxFfn& f, const void* x, hipStream_t stream) {
+  MxArgs a = mx_args<EPI>(ctx, f, 16 * TMX, NW * (EPI == EPI_H ? 32 : 64));
+  if (BF16)
+    for (MxProblem* p : {&a.dense, &a.grouped}) {
+      p->A = static_cast<const uint8_t*>(x);
+      p->a_row = static_cast<int64_t>(ctx->cfg.H) * 2;
+    }
+  KernelTimer timer(ctx, EPI == EPI_H ? REVIVE_K_MX_GATE_UP : REVIVE_K_MX_DOWN, stream);
+  return launch_mx_stream<TMX, 4, NW, EPI, BF16>(ctx, a, stream);
+}
+
+// Workgroups of four wavefronts, or of two where that leaves the busiest CU less to stream.  us of the FFN, four and two: 9
+// matrices of 7168 x 2048 (144 and 288 workgroups of gate/up: 4 and 4 wavefronts) 40 and 44, 33 (528 and 1056: 12 and 10) 138
+// and 122, 7 of 2048 x 1408 (88 and 176: 4 and 2) 20.7 and 16.4.
+template <int TMX, int EPI, bool BF16>
+int mx_stream_product(revive_ctx* ctx, const MxFfn& f, const void* x, hipStream_t stream) {
+  auto busiest = [&](int nw) {  // wavefronts
+    const MxArgs a = mx_args<EPI>(ctx, f, 16 * TMX, nw * (EPI == EPI_H ? 32 : 64));
+    return nw * ceil_div(a.dense.blocks + a.grouped.blocks, kMxCus);
+  };
+  if (busiest(2) < busiest(4)) return mx_stream_as<TMX, 2, EPI, BF16>(ctx, f, x, stream);
+  return mx_stream_as<TMX, 4, EPI, BF16>(ctx, f, x, stream);
 }
 
 int mx_tile_ffn(revive_ctx* ctx, const MxFfn& f, hipStream_t stream) {
@@ -92,12 +115,17 @@ int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
                          hipStream_t stream) {
   const revive_config& c = ctx->cfg;
   const Workspace& w = ctx->ws;
-  const int rc = launch_mx_quantize_tiled(ctx, x, T, c.H, ctx->d_ws + w.off_mx_x, ctx->d_ws + w.off_mx_x_scales, stream);
-  if (rc != REVIVE_OK) return rc;
   const MxFfn f{src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * c.k, y_shared ? T : 0};
+  if (T <= kMxFewTokens) {
+    const int rc = mx_stream_product<1, EPI_H, true>(ctx, f, x, stream);
+    return rc != REVIVE_OK ? rc : mx_stream_product<1, EPI_Y, false>(ctx, f, nullptr, stream);
+  }
+  int rc = launch_mx_quantize_tiled(ctx, x, T, c.H, ctx->d_ws + w.off_mx_x, ctx->d_ws + w.off_mx_x_scales, stream);
+  if (rc != REVIVE_OK) return rc;
   // The tiles address a row of x by 32 bits.
-  if (f.N > 64 * ctx->P && static_cast<int64_t>(T) * mx_code_row(c.H) < (1ll << 32)) return mx_tile_ffn(ctx, f, stream);
-  return mx_stream_ffn<4, 4, 4>(ctx, f, stream);
+  if (f.N > kMxTileRowsPerSlot * static_cast<int64_t>(ctx->P) && static_cast<int64_t>(T) * mx_code_row(c.H) < (1ll << 32)) return mx_tile_ffn(ctx, f, stream);
+  rc = mx_stream_product<4, EPI_H, false>(ctx, f, nullptr, stream);
+  return rc != REVIVE_OK ? rc : mx_stream_product<4, EPI_Y, false>(ctx, f, nullptr, stream);
 }
 
 }  // namespace revive

@@ -10,6 +10,9 @@
 // half of them gate, half up).  A block of weights (16 rows, 128 K-elements) is one KiB that the wavefront loads in address
 // order and feeds to the matrix cores as it is.  Activations come through LDS, 512 K-elements at a time, in two buffers.
 // What bounds it is how fast HBM is read: the next 512 K-elements of weights are on their way in registers.
+//
+// BF16: A is the bf16 rows themselves, and a thread rounds blocks of 32 numbers to 4 bits on their way to LDS.  Every workgroup
+// does that for its rows, which is less than a launch of its own for up to 16 tokens (kMxFewTokens).
 #pragma once
 
 #include <type_traits>
@@ -27,7 +30,7 @@ enum { EPI_H = 0, EPI_Y = 1 };
 __host__ __device__ inline int64_t mx_h_at(int s, int64_t rows, int64_t row) { return (static_cast<int64_t>(s >> 1) * rows + row) * 128 + (s & 1) * 64; }
 
 struct MxProblem {
-  const uint8_t* A;          // codes of row r, step s: A + r * a_row + s / 2 * a_pair + s % 2 * 64, 64 bytes
+  const uint8_t* A;          // codes of row r, step s: A + r * a_row + s / 2 * a_pair + s % 2 * 64, 64 bytes; BF16: row r at A + r * a_row
   int64_t a_row, a_pair;
   const uint8_t* A_scales;   // rows of mx_scale_row(K) bytes
   const int32_t* src_of;     // not null: row r of the product is row src_of[r] / k of A
@@ -73,14 +76,37 @@ __device__ __forceinline__ uint32_t mx_swiglu_codes(const mx_f32x4& g0, const mx
   return mx_codes(v, mx_scale_f32(byte));
 }
 
+// A block of 32 bf16 numbers -> four words of codes, and its scale byte.
+typedef uint32_t mx_u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ mx_u32x4 mx_block_codes(const mx_u32x4* x, uint32_t& byte) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x[i >> 2][i & 3] & 0x7FFF7FFFu));
+  byte = mx_scale_byte(static_cast<uint32_t>(m[0] > m[1] ? m[0] : m[1]) << 16);
+  const float scale = mx_scale_f32(byte);
+  mx_u32x4 o;
+  auto two = [](uint32_t v) { return __builtin_bit_cast(bf16x2, v); };
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, two(x[w][0]), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(x[w][1]), scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(x[w][2]), scale, 2);
+    o[w] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, two(x[w][3]), scale, 3);
+  }
+  return o;
+}
+
 template <typename F, int... S>
 __device__ __forceinline__ void mx_for(std::integer_sequence<int, S...>, F f) { (f(std::integral_constant<int, S>{}), ...); }
 
-template <int TMX, int W, int NW, int EPI>
+template <int TMX, int W, int NW, int EPI, bool BF16>
 __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
   constexpr int NT = 64 * NW, PAIRS = EPI == EPI_H ? W / 4 : W / 2;  // sets of 32 output columns per wavefront
   static_assert(PAIRS >= 1, "output columns in sets of 32");
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][TMX * 16 * 256];
+  constexpr int ROWS = TMX * 16 * 256;  // bytes of a buffer's codes; BF16: its scales, 16 bytes a row, follow
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][ROWS + (BF16 ? TMX * 256 : 0)];
   const bool dense = blockIdx.x < static_cast<unsigned>(a.dense.blocks);
   const MxProblem g = dense ? a.dense : a.grouped;
   const int b = dense ? blockIdx.x : blockIdx.x - a.dense.blocks;
@@ -135,39 +161,49 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     constexpr int WORDS = TM * 16 * 16;               // 16-byte words of one group of activations
     constexpr int NA = (WORDS + NT - 1) / NT;         // per thread
     const uint8_t* a_src[NA];
-    uint32_t a_dst[NA];
+    uint32_t a_dst[NA], s_dst[NA];
     int a_part[NA];
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
       const int w = (i * NT + tid) % WORDS;
       const int row = w >> 4, c = w & 15;
-      a_part[i] = c >> 2;
-      a_src[i] = g.A + source(row) * g.a_row + (c & 3) * 16;
+      a_part[i] = BF16 ? c : c >> 2;
+      a_src[i] = g.A + source(row) * g.a_row + (BF16 ? 0 : (c & 3) * 16);
       a_dst[i] = row * 256 + ((c ^ (row & 15)) << 4);
+      s_dst[i] = ROWS + row * 16 + mx_scale_at(c);
     }
     const uint8_t* x_src[TM];
+    if (!BF16)
 #pragma unroll
-    for (int i = 0; i < TM; ++i) x_src[i] = g.A_scales + source(i * 16 + r16) * mx_scale_row(g.K) + kb * 4;
+      for (int i = 0; i < TM; ++i) x_src[i] = g.A_scales + source(i * 16 + r16) * mx_scale_row(g.K) + kb * 4;
     mx_f32x4 acc[W][TM];
 #pragma unroll
     for (int s = 0; s < W; ++s)
 #pragma unroll
       for (int i = 0; i < TM; ++i) acc[s][i] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
 
-    mx_u32x4 wf[4][W], af[NA];
+    mx_u32x4 wf[4][W], af[NA][BF16 ? 4 : 1];
     uint32_t ws[W], xs[TM], ws_next[W], xs_next[TM];
     auto load_a = [&](int q) {
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
-        const int s = min(q * 4 + a_part[i], KT - 1);
-        af[i] = mx_load16(a_src[i] + (s >> 1) * g.a_pair + (s & 1) * 64);
+        if (BF16) {  // blocks past the row: the last one again, for weights of zero
+          const uint8_t* block = a_src[i] + min(q * 16 + a_part[i], g.K / kMxBlock - 1) * 64;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            af[i][w] = *reinterpret_cast<const __attribute__((address_space(1))) mx_u32x4_any*>(reinterpret_cast<uintptr_t>(block + w * 16));
+        } else {
+          const int s = min(q * 4 + a_part[i], KT - 1);
+          af[i][0] = mx_load16(a_src[i] + (s >> 1) * g.a_pair + (s & 1) * 64);
+        }
       }
     };
     auto load_scales = [&](int q, uint32_t* w, uint32_t* x) {
 #pragma unroll
       for (int s = 0; s < W; ++s) w[s] = mx_load4(B + s_off[s] + static_cast<int64_t>(q) * kMxPanelScales);
+      if (!BF16)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) x[i] = mx_load4(x_src[i] + q * 16);
+        for (int i = 0; i < TM; ++i) x[i] = mx_load4(x_src[i] + q * 16);
     };
     auto load_w = [&](int step, int h) {
       const uint8_t* wp = B + static_cast<int64_t>(min(step, KT - 1)) * kMxPanelStep;
@@ -179,7 +215,15 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     };
     auto stage = [&](int buf) {
 #pragma unroll
-      for (int i = 0; i < NA; ++i) *reinterpret_cast<mx_u32x4*>(lds[buf] + a_dst[i]) = af[i];
+      for (int i = 0; i < NA; ++i) {
+        if (BF16) {
+          uint32_t byte;
+          *reinterpret_cast<mx_u32x4*>(lds[buf] + a_dst[i]) = mx_block_codes(af[i], byte);
+          lds[buf][s_dst[i]] = static_cast<uint8_t>(byte);
+        } else {
+          *reinterpret_cast<mx_u32x4*>(lds[buf] + a_dst[i]) = af[i][0];
+        }
+      }
     };
     auto publish = [&]() {  // this wavefront's LDS accesses are done; then everybody's are
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -196,6 +240,9 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     publish();
     for (int q = 0; q < NG; ++q) {
       load_scales(min(q + 1, NG - 1), ws_next, xs_next);
+      if (BF16)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) xs[i] = *reinterpret_cast<const uint32_t*>(lds[q & 1] + ROWS + (i * 16 + r16) * 16 + kb * 4);
       mx_for(std::make_integer_sequence<int, 4>{}, [&](auto step) {
         constexpr int h = decltype(step)::value;
         if (q * 4 + h < KT) {
@@ -214,8 +261,9 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
       load_a(min(q + 2, NG - 1));
 #pragma unroll
       for (int s = 0; s < W; ++s) ws[s] = ws_next[s];
+      if (!BF16)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) xs[i] = xs_next[i];
+        for (int i = 0; i < TM; ++i) xs[i] = xs_next[i];
       publish();
     }
 
@@ -249,11 +297,11 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
   else run(std::integral_constant<int, TMX>{}, Y{});
 }
 
-template <int TMX, int W, int NW, int EPI>
+template <int TMX, int W, int NW, int EPI, bool BF16>
 int launch_mx_stream(revive_ctx* ctx, const MxArgs& args, hipStream_t stream) {
   const int grid = args.dense.blocks + args.grouped.blocks;
   if (grid <= 0) return REVIVE_OK;
-  hipLaunchKernelGGL((mx_stream_kernel<TMX, W, NW, EPI>), dim3(grid), dim3(64 * NW), 0, stream, args);
+  hipLaunchKernelGGL((mx_stream_kernel<TMX, W, NW, EPI, BF16>), dim3(grid), dim3(64 * NW), 0, stream, args);
   return check_hip(ctx, hipGetLastError(), "mx_stream launch");
 }
 
