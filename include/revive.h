@@ -351,7 +351,7 @@ int revive_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t ro
                          void* out, int64_t ld, revive_stream stream);
 
 /* Weights of the 4-bit FFN: codes and scales of an output-major matrix [rows, K]
- * (K a multiple of 32) into the order in which the kernels read them.
+ * (K a multiple of 32, rows * K < 2^32) into the order in which the kernels read them.
  * revive_mx_packed_bytes gives the size of `packed` (dev, 16-byte aligned).  Rows
  * are filled up with zeros to a multiple of 128.  Packed, a matrix is
  *   codes  [rows/128][ceil(K/128)][8][64][16 bytes]: blocks of 16 rows x 128 K;
@@ -368,7 +368,8 @@ int revive_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t rows, in
  * Q the rounding above along a row, for every slot p with rows [slot_offsets[p],
  * slot_offsets[p+1]):  h = Q(silu(Q(x) G_p) * (Q(x) U_p)),  y = h D_p, fp32 sums, and
  * the same on all T rows of x for the shared expert when y_shared != NULL.
- *   x          dev [T, H] bf16: the tokens, not permuted; quantised here, once each
+ *   x          dev [T, H] bf16: the tokens, not permuted; quantised here, at any
+ *              address that fits their elements
  *   src_of     dev int32 [N] (revive_dispatch_index): row r is token src_of[r] / k
  *   w_gate_up  dev table of P dev pointers: packed gate matrix [I, H] followed by
  *              the packed up matrix;  w_down: packed [H, I].  Entries of slots that

@@ -186,7 +186,8 @@ def check_ffn(y, x, w, what):
     off = np.abs(y - want)
     assert np.isfinite(y).all(), what
     assert (off <= allowed).all(), (what, float((off / allowed).max()), np.argwhere(off > allowed)[:4].tolist())
-    assert np.median(slack @ np.abs(w["down"])) <= 0.02 * np.sqrt(np.mean(want ** 2)) + 1e-30  # the allowance is the exception
+    if len(y) >= 8:  # the allowance is the exception (of fewer rows a single tie may make it the rule)
+        assert np.median(slack @ np.abs(w["down"])) <= 0.02 * np.sqrt(np.mean(want ** 2)) + 1e-30
 
 
 # hidden and intermediate sizes that end inside a step (128), a group of steps (512) and a panel of rows (128); slots with one
@@ -325,3 +326,58 @@ def test_ffn_refuses():
     fp32 = ReviveLayer(cfg)
     assert fp32.L.revive_mx_expert_ffn(fp32._ctx, *good) == -1
     fp32.close()
+
+
+# ---- which kernel serves a call does not show ----------------------------------------------------
+
+
+# few tokens (their rows are rounded on the way): row counts around its limit, slots with several row tiles, K that ends inside a
+# step and inside a group, workgroups of two wavefronts and of four (many slots and wide matrices)
+@pytest.mark.parametrize("H,I,I_shared,k,rows,T", [(64, 64, 0, 1, [1], 1), (1088, 192, 64, 3, [1, 0, 2], 1), (192, 576, 320, 3, [40, 0, 5], 15),
+                                                   (704, 64, 64, 3, [17, 16, 15], 16), (704, 64, 64, 3, [17, 17, 17], 17), (192, 512, 0, 20, [16] * 20, 16),
+                                                   (1088, 64, 64, 20, [16] * 20, 16), (192, 1024, 0, 8, [16] * 20, 40), (2112, 64, 64, 8, [16] * 20, 40)])
+def test_ffn_of_few_tokens(H, I, I_shared, k, rows, T):
+    f = Ffn(H, I, k, rows, I_shared, T, seed=H + T)
+    f.check(*f.run())
+    f.L.close()
+
+
+def test_ffn_of_few_tokens_that_are_not_finite():
+    f = Ffn(576, 128, 2, [9, 4, 0, 5], 64, seed=8)
+    clean, clean_shared = (f64(t) for t in f.run())
+    f.x[3, 570], f.x[7, 0] = float("nan"), -float("inf")
+    y, shared = (f64(t) for t in f.run())
+    touched = np.isin(f.src_of // 2, [3, 7])
+    assert np.isnan(y[touched]).all() and np.array_equal(y[~touched], clean[~touched])
+    others = [t for t in range(f.T) if t not in (3, 7)]
+    assert np.isnan(shared[[3, 7]]).all() and np.array_equal(shared[others], clean_shared[others])
+    f.L.close()
+
+
+@pytest.mark.parametrize("T", [5, 30, 300])
+def test_ffn_of_tokens_at_any_address(T):
+    f = Ffn(320, 64, 1, [T], 64, T, seed=T)
+    y, shared = f.run()
+    whole = torch.zeros(T * 320 + 8, dtype=torch.bfloat16, device="cuda")
+    for shift in (1, 3, 4):
+        x = whole[shift:shift + T * 320].view(T, 320)
+        x.copy_(f.x)
+        out = (torch.zeros_like(y), torch.zeros_like(shared))
+        f.L.mx_expert_ffn(x, f.d_src, f.d_offsets, T, *f.sh, out=out)
+        assert torch.equal(out[0], y) and torch.equal(out[1], shared)
+    f.L.close()
+
+
+def test_ffn_does_not_depend_on_the_token_count():
+    """The same tokens among more of them: every form of the kernels adds up in the same order."""
+    T = 600
+    f = Ffn(1088, 704, 1, [T], 576, T, seed=2)
+    f.src_of = np.arange(T, dtype=np.int32)
+    f.d_src = torch.from_numpy(f.src_of).cuda()
+    y, shared = f.run()
+    f.check(y, shared)
+    for n in (1, 2, 16, 17, 32, 33, 64, 255, 256, 257, 599):
+        offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        some, some_shared = f.L.mx_expert_ffn(f.x, f.d_src, offsets, n, *f.sh)
+        assert torch.equal(some, y[:n]) and torch.equal(some_shared, shared[:n]), n
+    f.L.close()
