@@ -261,9 +261,9 @@ _MX_DTYPE = {torch.float32: DTYPE["fp32"], torch.bfloat16: DTYPE["bf16"]}
 def _mx_check_form(codes: torch.Tensor, scales: torch.Tensor, rows: int, n: int):
     """codes [rows, 16 n] and scales [rows, n], contiguous uint8."""
     if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or codes.shape != (rows, 16 * n) or scales.shape != (rows, n)
-            or not codes.is_contiguous() or not scales.is_contiguous()):
+            or not codes.is_contiguous() or not scales.is_contiguous() or not codes.is_cuda or not scales.is_cuda):
         raise ValueError(f"codes {codes.dtype} {tuple(codes.shape)} and scales {scales.dtype} {tuple(scales.shape)}: contiguous uint8 "
-                         f"{(rows, 16 * n)} and {(rows, n)} expected")
+                         f"{(rows, 16 * n)} and {(rows, n)} in device memory expected")
 
 
 def _mx_rows(x: torch.Tensor, what: str):
@@ -272,8 +272,8 @@ def _mx_rows(x: torch.Tensor, what: str):
     if dtype is None:
         raise TypeError(f"{what}: microscaled numbers are made of and into float32 and bfloat16, not {x.dtype}")
     shape, stride = x.shape, x.stride()
-    if len(shape) != 2:
-        raise ValueError(f"{what} is a matrix")
+    if len(shape) != 2 or not x.is_cuda:
+        raise ValueError(f"{what} is a matrix in device memory")
     rows, K = shape
     ld = stride[0] if rows > 1 else K
     if ld < K or (K > 1 and stride[1] != 1):
@@ -490,6 +490,8 @@ class ReviveLayer:
     def route_biased(self, x, w_router, bias, T: int, renormalise=True, logits=None, logits_given=False, out=None, stream=None):
         """revive_route_biased: experts chosen by score + bias (fp32 [E]), weighted by the score."""
         k = self.cfg.k
+        if bias.dtype is not torch.float32 or bias.numel() != self.cfg.E or not bias.is_contiguous() or not bias.is_cuda:
+            raise ValueError(f"bias: {self.cfg.E} contiguous float32 in device memory expected")
         if logits is None:
             logits = self.empty(T, self.cfg.E, dtype=torch.float32)
         if out is None:
@@ -542,6 +544,8 @@ class ReviveLayer:
     def mx_expert_ffn(self, x, src_of, slot_offsets, T: int, w_sh_gate_up=None, w_sh_down=None, out=None, stream=None):
         """revive_mx_expert_ffn: (y_perm, y_shared) of the 4-bit experts; x [T, H] as it came, rows found through src_of."""
         assert self._mx_tabs is not None, "set_mx_expert_weights first"
+        if x.dtype is not torch.bfloat16 or not x.is_contiguous():
+            raise ValueError("x: contiguous rows of bfloat16 expected")
         use_shared = w_sh_gate_up is not None
         if out is None:
             out = (self.empty(T * self.cfg.k, self.cfg.H), self.empty(T, self.cfg.H) if use_shared else None)

@@ -13,7 +13,10 @@ namespace revive {
 namespace {
 
 constexpr int kMxCus = 256;
-// Up to so many tokens each workgroup of the first product rounds its rows of x itself.
+// Up to so many tokens, those that fit one row-tile of the shared expert, each workgroup of the first product rounds its rows of
+// x itself, which saves a launch.  us of the FFN, rounded on the way and by a launch of its own: 5
+// matrices of 1024 x 512 for a token 9.7 and 11.5, for 16 tokens 12.3 and 14.0; 2048 x 1408, a token 14.7 and 16.0, 16 tokens 49
+// and 45 to 51; 7168 x 2048, a token 40 and 42, 8 tokens 217 to 228 and 215, 16 tokens 373 and 357 to 377.
 constexpr int kMxFewTokens = 16;
 // Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below
 // it the streaming kernel, which starts sooner.  us, streaming and tiles: 288 slots, H = 7168, I = 2048: 14 rows 1146 and 1192,

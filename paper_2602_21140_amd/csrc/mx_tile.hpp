@@ -10,6 +10,11 @@
 // weights from HBM and 16 KiB of activations from the L2 take 0.69 us (256 CUs together), with 64 bytes of a row at a time
 // 0.85.  Results leave through LDS for the same reason, 64 or 128 bytes of a row by neighbouring lanes.
 //
+// us of the two products of 8192 tokens, 288 slots, H = 7168, I = 2048 (2.16e12 and 1.08e12 multiply-adds: 3.5 and 2.8 PFLOP/s;
+// 4.5 and 2.2 GB of weights): 1240 and 780; the copies alone 1070 and 680, everything but the copies 860 and 600, and what a
+// tile costs before its first and after its last step 210 and 320.  Weights that all slots share (so that no HBM is read) 1020
+// and 600.
+//
 // LDS: weights lie in operand order, as in memory.  Activation row r is at r * 128 bytes, its 16-byte chunk c at chunk
 // c ^ ((r >> 1) & 7): a fragment read (16 rows, four chunks) meets no bank twice in any of its four passes, whose lanes are 0-3,
 // 12-15, 20-27 and so on.

@@ -23,6 +23,8 @@ def test_quantize_refuses_before_any_launch():
     with pytest.raises(ValueError):
         mx_quantize(torch.zeros(64, 2).t())
     with pytest.raises(ValueError):
+        mx_quantize(torch.zeros(2, 64))  # not in device memory
+    with pytest.raises(ValueError):
         mx_dequantize(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 3, dtype=torch.uint8))
     lib = binding.lib()
     assert lib.revive_mx_quantize(None, 1, 4, 64, 64, None, None, None) == -1
