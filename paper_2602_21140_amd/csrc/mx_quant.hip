@@ -45,8 +45,8 @@ struct QuantArgs {
 // reads and writes in address order.  kUnits of them are in flight.  TILED: the scales' order is that of the kernels'
 // activations.
 //
-// Bound by HBM.  ONCE (rows larger than the last-level cache): non-temporal loads, here and for the way back non-temporal stores,
-// leave the caches to the codes.
+// Bound by HBM: 32 768 x 7168 bf16 to codes in 91 us (6.5 TB/s) and back in 84 (7.0).  ONCE (rows larger than the last-level cache):
+// non-temporal loads, here and for the way back non-temporal stores, leave the caches to the codes.
 constexpr int kUnits = 4;
 constexpr int64_t kOnceBytes = 256ll << 20;
 template <typename El, bool ONCE, bool TILED>
