@@ -75,6 +75,20 @@ __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, dpp_f<4>(v, kOut));
   return __int_as_float(last_lane(__float_as_int(fmaxf(v, dpp_f<5>(v, kOut)))));
 }
+constexpr int kLeast = -2147483647 - 1;  // changes no maximum, so that a step is one instruction
+__device__ __forceinline__ int wave_max(int v) {
+  v = max(v, dpp<0>(v, kLeast));
+  v = max(v, dpp<1>(v, kLeast));
+  v = max(v, dpp<2>(v, kLeast));
+  v = max(v, dpp<3>(v, kLeast));
+  v = max(v, dpp<4>(v, kLeast));
+  return last_lane(max(v, dpp<5>(v, kLeast)));
+}
+// An integer that is ordered as the float is (which is neither NaN nor -0).
+__device__ __forceinline__ int ordered(float v) {
+  const int b = __float_as_int(v);
+  return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
 __device__ __forceinline__ float wave_sum(float v) {
   v = row_sum(v);
   v += dpp_f<4>(v, 0.f);
@@ -124,7 +138,7 @@ __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j
 // experts j, j + lg, ..., or with WIDE (E a multiple of 64, 16-byte loads) its words of four j, j + lg, ...
 //
 // Bound by the ALU: 8192 tokens of 256 experts in 8 groups, k = 8, 7.7 us (1.2 TB/s), 32 768 of 384 experts 21.2 (2.5 TB/s); with a
-// wavefront per token 20.4 and 42.7.  What a choice costs is kept small by two levels: a lane has the best key of every four of its experts in
+// wavefront per token 12.9 and 36.  What a choice costs is kept small by two levels: a lane has the best key of every four of its experts in
 // registers and the keys in LDS; a round looks at the bests, and the four keys of the winning one are read, stripped of the
 // winner and put back.
 template <int V, bool GROUPED, bool WIDE>
@@ -253,7 +267,7 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
 }
 
 // A wavefront per token; lane l holds experts l, l + 64, ...  Bound by latency: the choices follow one another, each a maximum over
-// the wavefront.  64 tokens of 256 experts in 8 groups, k = 8, 6.4 us.
+// the wavefront.  64 tokens of 256 experts in 8 groups, k = 8, 6.0 us; 512 of 512 experts, k = 16, 8.1.
 template <int V>
 __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   const int lane = threadIdx.x & 63;
@@ -345,26 +359,30 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
     }
   }
 
-  // k rounds of arg-max (largest key, ties to the lower expert id); lane j keeps the j-th choice
-  int my_e = 0;
+  // k rounds of arg-max (largest key, ties to the lower expert id); lane j keeps the j-th choice.  Keys as integers of the same
+  // order, whose maxima take the other lane's as an operand; a lane has its best, u, and which of its experts that is, so that
+  // several lanes with the round's best are the only ones whose ids have to be compared.
+  int place[V], u = 0, ui = 0, my_e = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) place[i] = ordered(key[i]);
 #pragma unroll 1
   for (int j = 0; j < p.k; ++j) {
-    float u = key[0];
+    u = place[0];
+    ui = 0;
 #pragma unroll
-    for (int i = 1; i < V; ++i) u = fmaxf(u, key[i]);
-    const float best = wave_max(u);
-    int wi = 0;
-    unsigned long long holders = 1ull;
-#pragma unroll
-    for (int i = V - 1; i >= 0; --i) {
-      const unsigned long long b = __ballot(key[i] == best);
-      if (b) { holders = b; wi = i; }
+    for (int i = 1; i < V; ++i) {
+      ui = place[i] > u ? i : ui;
+      u = max(u, place[i]);
     }
-    const int w = __builtin_ctzll(holders);
+    const int best = wave_max(u);
+    const unsigned long long holders = __ballot(u == best);
+    int w = __builtin_ctzll(holders);
+    if (holders & (holders - 1)) w = -wave_max(u == best ? -(ui * 64 + lane) : -64 * V) & 63;
+    const int e = __builtin_amdgcn_readlane(ui, w) * 64 + w;
+    const int taken = lane == w ? ui : -1;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (wi == i && lane == w) key[i] = kOut;
-    if (lane == j) my_e = min(wi * 64 + w, p.E - 1);
+    for (int i = 0; i < V; ++i) place[i] = taken == i ? ordered(kOut) : place[i];
+    if (lane == j) my_e = min(e, p.E - 1);
   }
 
   const float zc = z[my_e];
@@ -377,10 +395,11 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
 
 // Which kernel.  A row of lanes per token does a quarter of the work, but one after the other: it wins once a wavefront per token
 // keeps the ALUs busy, later where experts are no multiple of 64 and its loads are of four bytes.  us in a graph, a row and a
-// wavefront per token: 256 experts in 8 groups, k = 8, 1024 tokens 6.7 and 6.7, 2048 6.8 and 7.4, 8192 7.9 and 14.3; 384, k = 8,
-// 1024 6.5 and 6.2, 2048 6.6 and 6.9, 8192 7.7 and 12.1; 512, k = 16, 1024 10.6 and 9.9, 2048 10.7 and 11.8; 64, k = 2, 2048
-// 3.2 and 2.8, 4096 3.2 and 3.5; 100, k = 4, 4096 5.0 and 4.4, 8192 5.4 and 5.6; 500, k = 8, 4096 12.0 and 10.5, 8192 13.2 and 16.5.
-constexpr int kRowsFrom = 2048, kNarrowRowsFrom = 6144;
+// wavefront per token: 256 experts in 8 groups, k = 8, 1024 tokens 6.7 and 6.2, 2048 6.8 and 6.9, 3000 6.8 and 7.9, 8192 7.9 and
+// 12.9; 384, k = 8, 2048 6.6 and 6.1, 3000 6.7 and 6.6, 8192 7.7 and 9.9; 512, k = 16, 2048 10.7 and 9.2, 3000 10.8 and 10.4, 4096
+// 10.9 and 11.7; 64, k = 2, 3000 3.2 and 3.0, 4096 3.2 and 3.4; 100, k = 4, 4096 5.0 and 4.1, 8192 5.4 and 5.1; 500, k = 8, 6144
+// 13.0 and 11.0, 8192 13.2 and 13.1.
+constexpr int kRowsFrom = 3000, kNarrowRowsFrom = 8192;
 // Workgroups of the rows' kernel at most; beyond them each takes its share of tokens.  32768 tokens, 384 experts: 512 26.7, 1024
 // 21.4, 2048 22.2.
 constexpr int kRowsWorkgroups = 1024;

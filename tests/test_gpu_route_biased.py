@@ -87,6 +87,18 @@ def test_many_tokens(E, n_group, topk_group, k):
     test_against_the_oracle(E, n_group, topk_group, k, "sigmoid" if k % 2 else "softmax", 6147)
 
 
+@pytest.mark.parametrize("E,n_group,topk_group,k", [(16, 1, 1, 2), (61, 1, 1, 1), (65, 1, 1, 16), (48, 4, 2, 3), (208, 2, 1, 8), (400, 2, 1, 8),
+                                                    (500, 1, 1, 16), (511, 1, 1, 5)])
+def test_a_row_of_lanes_per_token(E, n_group, topk_group, k):
+    test_against_the_oracle(E, n_group, topk_group, k, "softmax" if k % 2 else "sigmoid", 8195)
+
+
+@pytest.mark.parametrize("T", [2999, 3000])
+@pytest.mark.parametrize("E,n_group,topk_group,k", [(256, 8, 4, 8), (320, 1, 1, 16), (512, 2, 1, 12)])
+def test_both_sides_of_the_kernels_line(E, n_group, topk_group, k, T):
+    test_against_the_oracle(E, n_group, topk_group, k, "softmax", T)
+
+
 def test_more_tokens_than_the_workgroups_take_at_once():
     test_against_the_oracle(64, 1, 1, 4, "softmax", 33001)
 
