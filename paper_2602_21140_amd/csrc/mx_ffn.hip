@@ -15,8 +15,8 @@ namespace {
 constexpr int kMxCus = 256;
 // Up to so many tokens, those that fit one row-tile of the shared expert, each workgroup of the first product rounds its rows of
 // x itself, which saves a launch.  us of the FFN, rounded on the way and by a launch of its own: 5
-// matrices of 1024 x 512 for a token 9.7 and 11.5, for 16 tokens 12.3 and 14.0; 2048 x 1408, a token 14.7 and 16.0, 16 tokens 49
-// and 45 to 51; 7168 x 2048, a token 40 and 42, 8 tokens 217 to 228 and 215, 16 tokens 373 and 357 to 377.
+// matrices of 1024 x 512 for a token 8.7 and 11.5, for 16 tokens 12.3 and 14.0; 2048 x 1408, a token 14.0 and 16.0, 16 tokens 49
+// and 45 to 51; 7168 x 2048, a token 39.5 and 42, 8 tokens 217 to 228 and 215, 16 tokens 373 and 357 to 377.
 constexpr int kMxFewTokens = 16;
 // Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below
 // it the streaming kernel, which starts sooner.  us, streaming and tiles: 288 slots, H = 7168, I = 2048: 14 rows 1146 and 1192,
@@ -90,13 +90,17 @@ int mx_stream_as(revive_ctx* ctx, const MxFfn& f, const void* x, hipStream_t str
 
 // Workgroups of four wavefronts, or of two where that leaves the busiest CU less to stream.  us of the FFN, four and two: 9
 // matrices of 7168 x 2048 (144 and 288 workgroups of gate/up: 4 and 4 wavefronts) 40 and 44, 33 (528 and 1056: 12 and 10) 138
-// and 122, 7 of 2048 x 1408 (88 and 176: 4 and 2) 20.7 and 16.4.
+// and 122, 7 of 2048 x 1408 (88 and 176: 4 and 2) 20.7 and 16.4.  Of one, whose lanes round four times as much, with few rows
+// only; one and the better of the others: a token, 9 matrices of 7168 x 2048 39.5 and 41, 7 of 2048 x 1408 14.0 and 15.0, 5 of
+// 1024 x 512 8.7 and 10.2; two tokens, 17 of 7168 x 2048 63 to 70 and 74, 13 of 2048 x 1408 17.5 and 19.4.
 template <int TMX, int EPI, bool BF16>
 int mx_stream_product(revive_ctx* ctx, const MxFfn& f, const void* x, hipStream_t stream) {
   auto busiest = [&](int nw) {  // wavefronts
     const MxArgs a = mx_args<EPI>(ctx, f, 16 * TMX, nw * (EPI == EPI_H ? 32 : 64));
     return nw * ceil_div(a.dense.blocks + a.grouped.blocks, kMxCus);
   };
+  if (TMX == 1 && f.N <= kMxFewRows * ctx->cfg.k && busiest(1) < busiest(2) && busiest(1) < busiest(4))
+    return mx_stream_as<TMX, TMX == 1 ? 1 : 2, EPI, BF16>(ctx, f, x, stream);  // of TMX > 1 there is none
   if (busiest(2) < busiest(4)) return mx_stream_as<TMX, 2, EPI, BF16>(ctx, f, x, stream);
   return mx_stream_as<TMX, 4, EPI, BF16>(ctx, f, x, stream);
 }

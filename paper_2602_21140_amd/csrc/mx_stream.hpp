@@ -10,7 +10,7 @@
 // half of them gate, half up).  A block of weights (16 rows, 128 K-elements) is one KiB that the wavefront loads in address
 // order and feeds to the matrix cores as it is.  Activations come through LDS, 512 K-elements at a time, in two buffers.
 // What bounds it is how fast HBM is read: the next 512 K-elements of weights are on their way in registers.  64 tokens on 237
-// matrices of H = 7168, I = 2048: gate and up in 525 us (7.0 TB/s), down in 285 (6.5); one token on 9 of them 27 and 12 (5.3 and
+// matrices of H = 7168, I = 2048: gate and up in 525 us (7.0 TB/s), down in 285 (6.5); one token on 9 of them 26 and 12 (5.4 and
 // 5.8: workgroups start and end together).
 //
 // BF16: A is the bf16 rows themselves, and a thread rounds blocks of 32 numbers to 4 bits on their way to LDS.  Every workgroup
@@ -27,6 +27,10 @@
 namespace revive {
 
 enum { EPI_H = 0, EPI_Y = 1 };
+
+// Of a row-tile with up to so many rows no more are copied and rounded; the other lanes multiply what the LDS holds, for results
+// that are not stored.
+constexpr int kMxFewRows = 4;
 
 // h, the activations of the second product: [pairs of steps][rows][128 bytes]; where the 64 bytes of step s of a row begin.
 __host__ __device__ inline int64_t mx_h_at(int s, int64_t rows, int64_t row) { return (static_cast<int64_t>(s >> 1) * rows + row) * 128 + (s & 1) * 64; }
@@ -157,10 +161,10 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     return g.src_of ? g.src_of[row] / g.k : row;
   };
 
-  auto run = [&](auto tm_tag, auto once_tag) {
+  auto run = [&](auto tm_tag, auto once_tag, auto rows_tag) {
     constexpr int TM = decltype(tm_tag)::value;
     constexpr bool ONCE = decltype(once_tag)::value;  // streamed past the caches' retention (non-temporal)
-    constexpr int WORDS = TM * 16 * 16;               // 16-byte words of one group of activations
+    constexpr int WORDS = decltype(rows_tag)::value * 16;  // 16-byte words of one group of activations
     constexpr int NA = (WORDS + NT - 1) / NT;         // per thread
     const uint8_t* a_src[NA];
     uint32_t a_dst[NA], s_dst[NA];
@@ -293,10 +297,12 @@ __global__ __launch_bounds__(64 * NW, 2) void mx_stream_kernel(MxArgs a) {
     }
   };
   using Y = std::true_type;
-  if (!once) run(std::integral_constant<int, TMX>{}, std::false_type{});
-  else if (TMX == 1 || rows <= 16) run(std::integral_constant<int, 1>{}, Y{});
-  else if (TMX == 2 || rows <= 32) run(std::integral_constant<int, (TMX < 2 ? TMX : 2)>{}, Y{});
-  else run(std::integral_constant<int, TMX>{}, Y{});
+  auto tiles = [&](auto tm, auto once_tag) { run(tm, once_tag, std::integral_constant<int, 16 * decltype(tm)::value>{}); };
+  if (!once) tiles(std::integral_constant<int, TMX>{}, std::false_type{});
+  else if (TMX == 1 && rows <= kMxFewRows) run(std::integral_constant<int, 1>{}, Y{}, std::integral_constant<int, kMxFewRows>{});
+  else if (TMX == 1 || rows <= 16) tiles(std::integral_constant<int, 1>{}, Y{});
+  else if (TMX == 2 || rows <= 32) tiles(std::integral_constant<int, (TMX < 2 ? TMX : 2)>{}, Y{});
+  else tiles(std::integral_constant<int, TMX>{}, Y{});
 }
 
 template <int TMX, int W, int NW, int EPI, bool BF16>

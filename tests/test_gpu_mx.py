@@ -342,6 +342,17 @@ def test_ffn_of_few_tokens(H, I, I_shared, k, rows, T):
     f.L.close()
 
 
+# up to four rows of a row-tile, and more of them in one slot than there are tokens; workgroups of one wavefront (sizes that would
+# leave some CUs twice the work with two)
+@pytest.mark.parametrize("H,I,I_shared,k,rows,T", [(64, 64, 64, 1, [1], 1), (64, 64, 0, 3, [4, 0, 5], 3), (192, 320, 64, 3, [0, 12, 0], 4),
+                                                   (576, 704, 192, 4, [3, 5, 0, 4, 8], 5), (1600, 704, 0, 20, [4] * 20, 4),
+                                                   (1600, 704, 64, 20, [40, 0, 37] + [0] * 17, 4)])
+def test_ffn_of_few_rows(H, I, I_shared, k, rows, T):
+    f = Ffn(H, I, k, rows, I_shared, T, seed=I + T)
+    f.check(*f.run())
+    f.L.close()
+
+
 def test_ffn_of_few_tokens_that_are_not_finite():
     f = Ffn(576, 128, 2, [9, 4, 0, 5], 64, seed=8)
     clean, clean_shared = (f64(t) for t in f.run())
@@ -376,7 +387,7 @@ def test_ffn_does_not_depend_on_the_token_count():
     f.d_src = torch.from_numpy(f.src_of).cuda()
     y, shared = f.run()
     f.check(y, shared)
-    for n in (1, 2, 16, 17, 32, 33, 64, 255, 256, 257, 599):
+    for n in (1, 2, 4, 5, 16, 17, 32, 33, 64, 255, 256, 257, 599):
         offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda")
         some, some_shared = f.L.mx_expert_ffn(f.x, f.d_src, offsets, n, *f.sh)
         assert torch.equal(some, y[:n]) and torch.equal(some_shared, shared[:n]), n
