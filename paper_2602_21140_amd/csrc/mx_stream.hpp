@@ -10,8 +10,8 @@
 // half of them gate, half up).  A block of weights (16 rows, 128 K-elements) is one KiB that the wavefront loads in address
 // order and feeds to the matrix cores as it is.  Activations come through LDS, 512 K-elements at a time, in two buffers.
 // What bounds it is how fast HBM is read: the next 512 K-elements of weights are on their way in registers.  64 tokens on 237
-// matrices of H = 7168, I = 2048: gate and up in 525 us (7.0 TB/s), down in 285 (6.5); one token on 9 of them 26 and 12 (5.4 and
-// 5.8: workgroups start and end together).
+// matrices of H = 7168, I = 2048: gate and up in 525 us (7.0 TB/s), down in 285 (6.5); one token on 9 of them 25 and 12
+// (5.7 in both: workgroups start and end together).
 //
 // BF16: A is the bf16 rows themselves, and a thread rounds blocks of 32 numbers to 4 bits on their way to LDS.  Every workgroup
 // does that for its rows, which is less than a launch of its own for up to 16 tokens (kMxFewTokens).
