@@ -2,8 +2,11 @@
 //
 // Paper: Sec. 2.1 (each expert acts as an FFN).  With Q the rounding of mx.hpp, every slot p with rows
 // [slot_offsets[p], slot_offsets[p+1]) computes h = Q(silu(Q(x) G_p) * (Q(x) U_p)), y = h D_p, and the shared expert the same on
-// all tokens.  x is quantised once per token; a routed row reads its token's codes through src_of, so that dispatch need not
+// all tokens.  x is quantised once per token, or where tokens are few by who multiplies it; a routed row reads its token's codes through src_of, so that dispatch need not
 // copy rows.  Slots without rows produce no tile and their weights are never read.
+#include <algorithm>
+
+#include "ctx.hpp"
 #include "mx_quant.hpp"
 #include "mx_stream.hpp"
 #include "mx_tile.hpp"
@@ -13,11 +16,15 @@ namespace revive {
 namespace {
 
 constexpr int kMxCus = 256;
-// Up to so many tokens, those that fit one row-tile of the shared expert, each workgroup of the first product rounds its rows of
-// x itself, which saves a launch.  us of the FFN, rounded on the way and by a launch of its own: 5
-// matrices of 1024 x 512 for a token 8.7 and 11.5, for 16 tokens 12.3 and 14.0; 2048 x 1408, a token 14.0 and 16.0, 16 tokens 49
-// and 45 to 51; 7168 x 2048, a token 39.5 and 42, 8 tokens 217 to 228 and 215, 16 tokens 373 and 357 to 377.
-constexpr int kMxFewTokens = 16;
+// With few tokens each workgroup of the first product rounds its rows of x itself, 16 at most, which saves a launch.  us of the
+// FFN, rounded on the way and by a launch of its own: 5 matrices of 1024 x 512 for a token 8.7 and 11.5, for 16 tokens 12.3 and
+// 14.0; 2048 x 1408, a token 14.0 and 16.0, 16 tokens 49 and 45 to 51; 7168 x 2048, a token 39.5 and 42, 8 tokens 217 to 228 and
+// 215, 16 tokens 373 and 357 to 377.  Of more tokens a slot may have several row-tiles, which a launch of some microseconds
+// outweighs where there is little to stream in all: 40 slots of 1024 x 512, 32 tokens 13.1 and 14.8, 64 13.1 and 16.8, 128 14.5 and
+// 16.0; 72 of 2048 x 1408, 32 tokens 53 and 57, 64 61 and 64, 128 66 and 64; 128 of 4096 x 256, 64 tokens 47 and 52; but 288 of
+// 7168 x 2048 (6 GB), 32 tokens 620 and 588, 64 863 and 866.
+constexpr int kMxFewTokens = 16, kMxFewTokensSmall = 64;
+constexpr int64_t kMxSmallBytes = 1ll << 30;
 // Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below
 // it the streaming kernel, which starts sooner.  us, streaming and tiles: 288 slots, H = 7168, I = 2048: 14 rows 1146 and 1192,
 // 28 rows 1276 and 1242, 57 rows 1426 and 1329; 72 slots, H = 2048, I = 1408: 21 rows 73 and 75, 43 rows 83 and 82; 40 slots, H =
@@ -123,7 +130,8 @@ int launch_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
   const revive_config& c = ctx->cfg;
   const Workspace& w = ctx->ws;
   const MxFfn f{src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * c.k, y_shared ? T : 0};
-  if (T <= kMxFewTokens) {
+  const int64_t streamed = static_cast<int64_t>(std::min(f.N, ctx->P)) * (2 * mx_packed_bytes(c.I, c.H) + mx_packed_bytes(c.H, c.I));
+  if (T <= kMxFewTokens || (T <= kMxFewTokensSmall && streamed <= kMxSmallBytes)) {
     const int rc = mx_stream_product<1, EPI_H, true>(ctx, f, x, stream);
     return rc != REVIVE_OK ? rc : mx_stream_product<1, EPI_Y, false>(ctx, f, nullptr, stream);
   }

@@ -14,7 +14,7 @@
 // (5.7 in both: workgroups start and end together).
 //
 // BF16: A is the bf16 rows themselves, and a thread rounds blocks of 32 numbers to 4 bits on their way to LDS.  Every workgroup
-// does that for its rows, which is less than a launch of its own for up to 16 tokens (kMxFewTokens).
+// does that for its rows, which with few tokens is less than a launch of its own (kMxFewTokens).
 #pragma once
 
 #include <type_traits>

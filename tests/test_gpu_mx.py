@@ -392,3 +392,61 @@ def test_ffn_does_not_depend_on_the_token_count():
         some, some_shared = f.L.mx_expert_ffn(f.x, f.d_src, offsets, n, *f.sh)
         assert torch.equal(some, y[:n]) and torch.equal(some_shared, shared[:n]), n
     f.L.close()
+
+
+# more tokens than are rounded on the way and few rows per slot: tiles of 64 rows, slots with one of 16, 32 and 64 rows and with
+# several, workgroups of two wavefronts and of four
+@pytest.mark.parametrize("H,I,I_shared,k,rows,T", [(192, 1024, 0, 8, [28] * 20, 70), (2112, 64, 64, 8, [28] * 20, 70), (576, 704, 192, 2, [64, 65, 0, 1, 16, 17, 33], 98),
+                                                   (64, 64, 0, 1, [1] * 65, 65), (1088, 320, 64, 3, [90, 0, 0, 0, 0, 100, 0, 5], 65)])
+def test_ffn_of_few_rows_per_slot(H, I, I_shared, k, rows, T):
+    f = Ffn(H, I, k, rows, I_shared, T, seed=H + len(rows))
+    f.check(*f.run())
+    f.L.close()
+
+
+def test_ffn_of_few_rows_per_slot_that_are_not_finite_and_at_any_address():
+    f = Ffn(576, 128, 1, [30, 40, 0, 10, 20], 64, 100, seed=12)
+    clean, clean_shared = (f64(t) for t in f.run())
+    whole = torch.zeros(100 * 576 + 8, dtype=torch.bfloat16, device="cuda")
+    x = whole[3:3 + 100 * 576].view(100, 576)
+    x.copy_(f.x)
+    x[3, 570], x[71, 0] = float("nan"), -float("inf")
+    y, shared = (f64(t) for t in f.L.mx_expert_ffn(x, f.d_src, f.d_offsets, 100, *f.sh))
+    touched = np.isin(f.src_of, [3, 71])
+    assert np.isnan(y[touched]).all() and np.array_equal(y[~touched], clean[~touched])
+    others = [t for t in range(100) if t not in (3, 71)]
+    assert np.isnan(shared[[3, 71]]).all() and np.array_equal(shared[others], clean_shared[others])
+    f.L.close()
+
+
+def test_ffn_does_not_depend_on_the_token_count_with_many_slots():
+    """As above where slots without rows keep the average per slot low."""
+    T = 200
+    f = Ffn(1088, 704, 1, [0, T, 0, 0, 0, 0, 0, 0], 576, T, seed=3)
+    f.src_of = np.arange(T, dtype=np.int32)
+    f.d_src = torch.from_numpy(f.src_of).cuda()
+    y, shared = f.run()
+    f.check(y, shared)
+    for n in (1, 16, 17, 64, 65, 128, 199):
+        offsets = torch.tensor([0, 0] + [n] * 7, dtype=torch.int32, device="cuda")
+        some, some_shared = f.L.mx_expert_ffn(f.x, f.d_src, offsets, n, *f.sh)
+        assert torch.equal(some, y[:n]) and torch.equal(some_shared, shared[:n]), n
+    f.L.close()
+
+
+def test_ffn_of_few_tokens_and_many_bytes():
+    """A layer too large for its tokens to be rounded on the way: the same bits as with fewer of them."""
+    P, H, I, T = 96, 5120, 2048, 48
+    cfg = SimpleNamespace(T=T, H=H, E=P, k=2, I=I, I_shared=0, n_ranks=1, slots_per_rank=P, max_replicas=1, score_fn="softmax", n_group=1,
+                          topk_group=1, dtype="bf16")
+    L = ReviveLayer(cfg)
+    gen = torch.Generator().manual_seed(1)
+    g, d = mx_pack_expert(*((torch.randn(s, generator=gen) * H ** -0.5).cuda() for s in ((H, I), (H, I), (I, H))))
+    L.set_mx_expert_weights([g] * P, [d] * P)
+    x = torch.randn(T, H, generator=gen).bfloat16().cuda()
+    src_of = torch.arange(2 * T, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([0] + [min(2 * T, 5 * (p // 4 + 1)) for p in range(P)], dtype=torch.int32, device="cuda")
+    y, _ = L.mx_expert_ffn(x, src_of, offsets, T)
+    few, _ = L.mx_expert_ffn(x[:12].contiguous(), src_of, offsets.clamp(max=24), 12)
+    assert bool(few.any(dim=1).all()) and torch.equal(y[:24], few)
+    L.close()
