@@ -107,19 +107,27 @@ __device__ __forceinline__ void top2_step(float& m1, float& m2) {
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float near_exp(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * kLog2e); }
 __device__ __forceinline__ float near_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2e)); }
-// The weights' scores, of the chosen experts: exp(x) for x in [-100, 88] with what the rounding of p left out.
-__device__ __forceinline__ float exp_of(float x) {
+// The weights' scores, of the chosen experts: exp(x + more) for x in [-100, 88] and a small rest, with what the rounding of p left
+// out.  The instruction has zero for what is below the least normal number, 2^-126.
+__device__ __forceinline__ float exp_of(float x, float more) {
   const float p = x * kLog2e, rest = fmaf(x, kLog2e, -p) + x * 1.92596299e-8f;  // log2(e) = kLog2e + 1.92596299e-8
   const float e = __builtin_amdgcn_exp2f(p);
-  return fmaf(e, rest * 0.693147181f, e);
+  return fmaf(e, fmaf(rest, 0.693147181f, more), e);
 }
-__device__ __forceinline__ float exp_below(float z, float m) {  // exp(-100) is zero in fp32
-  const float d = z - m;
-  return exp_of(d < -100.f ? -100.f : d);
+// exp(z - m), z <= m, of the difference and what its rounding left out; -100 stands for all that make zero.
+__device__ __forceinline__ float exp_below(float z, float m) {
+  const float d = z - m, t = d - z, more = (z - (d - t)) - (m + t);
+  return d < -100.f ? exp_of(-100.f, 0.f) : exp_of(d, more);
+}
+// Softmax scores of the chosen experts, `shift` and `scale` being those of the row.  Renormalised, what a score shares with the
+// others goes out, and it is taken from the largest chosen logit, `top`: a larger one that is lost, or kept back by the bias,
+// would leave nothing but zeros of scores 87 below it.  A row whose scores are NaN has `scale` NaN.
+__device__ __forceinline__ float softmax_chosen(float z, float top, float shift, float scale, bool renormalise) {
+  return exp_below(z, renormalise ? top : shift) * scale;
 }
 __device__ __forceinline__ float sigmoid(float z) {
   const float x = z < -87.f ? -87.f : z > 87.f ? 87.f : z;
-  return __builtin_amdgcn_rcpf(1.0f + exp_of(-x));
+  return __builtin_amdgcn_rcpf(1.0f + exp_of(-x, 0.f));
 }
 
 __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j, int e, float weight) {
@@ -260,7 +268,7 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
     }
     my_e = min(my_e, p.E - 1);
     const float zc = z[my_e];
-    const float sc = sig ? sigmoid(zc) : exp_below(zc, shift) * scale;
+    const float sc = sig ? sigmoid(zc) : softmax_chosen(zc, row_max(li < p.k ? zc : kOut), shift, scale, p.renormalise);
     const float total = p.renormalise ? row_sum(li < p.k ? sc : 0.f) : 1.f;
     if (li < p.k && t < p.T) store_choice(p, t, li, my_e, sc / total * p.route_scale);
   }
@@ -386,7 +394,7 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   }
 
   const float zc = z[my_e];
-  const float sc = sig ? sigmoid(zc) : exp_below(zc, shift) * scale;
+  const float sc = sig ? sigmoid(zc) : softmax_chosen(zc, wave_max(lane < p.k ? zc : kOut), shift, scale, p.renormalise);
   const float sum = p.renormalise ? wave_sum(lane < p.k ? sc : 0.f) : 1.f;
   if (lane < p.k) store_choice(p, t, lane, my_e, sc / sum * p.route_scale);
 }
