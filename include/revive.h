@@ -250,8 +250,9 @@ int revive_route(revive_ctx* ctx, const void* x, const void* w_router, float* lo
  *              keys closer than their rounding may swap.
  *   n_group > 1: a group scores the sum of its two best keys above -inf, in fp32.
  *   topk_weight: the chosen expert's score (without the bias); renormalise != 0:
- *              over the sum of the chosen scores, as exact where softmax scores
- *              are too small for fp32; then times route_scale.
+ *              over the sum of the chosen scores, as exact where these are too
+ *              small for fp32 (a row of nothing but scores of logits -inf: 0 / 0,
+ *              NaN); otherwise a score below 2^-126 is 0.  Then times route_scale.
  * A key that is NaN or -inf orders nothing: its expert counts as absent while
  * live experts with other keys are left, in its group's score too, and is chosen
  * after them, in ascending id (the weight of a NaN score is NaN; renormalised, so

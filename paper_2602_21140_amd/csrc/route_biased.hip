@@ -125,9 +125,10 @@ __device__ __forceinline__ float exp_below(float z, float m) {
 __device__ __forceinline__ float softmax_chosen(float z, float top, float shift, float scale, bool renormalise) {
   return exp_below(z, renormalise ? top : shift) * scale;
 }
-__device__ __forceinline__ float sigmoid(float z) {
-  const float x = z < -87.f ? -87.f : z > 87.f ? 87.f : z;
-  return __builtin_amdgcn_rcpf(1.0f + exp_of(-x, 0.f));
+// Sigmoid scores.  Below -30 a score is exp(z) to all bits of fp32; where all chosen ones are, they are renormalised as above.
+__device__ __forceinline__ float sigmoid_chosen(float z, float top, bool renormalise) {
+  if (z < -30.f) return exp_below(z, renormalise && top < -30.f ? top : 0.f);
+  return __builtin_amdgcn_rcpf(1.0f + exp_of(z > 87.f ? -87.f : -z, 0.f));
 }
 
 __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j, int e, float weight) {
@@ -268,7 +269,8 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
     }
     my_e = min(my_e, p.E - 1);
     const float zc = z[my_e];
-    const float sc = sig ? sigmoid(zc) : softmax_chosen(zc, row_max(li < p.k ? zc : kOut), shift, scale, p.renormalise);
+    const float top = row_max(li < p.k ? zc : kOut);
+    const float sc = sig ? sigmoid_chosen(zc, top, p.renormalise) : softmax_chosen(zc, top, shift, scale, p.renormalise);
     const float total = p.renormalise ? row_sum(li < p.k ? sc : 0.f) : 1.f;
     if (li < p.k && t < p.T) store_choice(p, t, li, my_e, sc / total * p.route_scale);
   }
@@ -394,7 +396,8 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   }
 
   const float zc = z[my_e];
-  const float sc = sig ? sigmoid(zc) : softmax_chosen(zc, wave_max(lane < p.k ? zc : kOut), shift, scale, p.renormalise);
+  const float top = wave_max(lane < p.k ? zc : kOut);
+  const float sc = sig ? sigmoid_chosen(zc, top, p.renormalise) : softmax_chosen(zc, top, shift, scale, p.renormalise);
   const float sum = p.renormalise ? wave_sum(lane < p.k ? sc : 0.f) : 1.f;
   if (lane < p.k) store_choice(p, t, lane, my_e, sc / sum * p.route_scale);
 }

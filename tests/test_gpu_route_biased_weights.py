@@ -47,3 +47,33 @@ def test_softmax_weights_far_below_an_expert_that_is_not_chosen(E, T):
         assert (np.abs(w - want) <= 16 * 2.0 ** -24 * want).all(), gap
         w, z, s = weights(E, T, 6, "softmax", logits, lost, False, seed=E)
         assert (np.abs(w - s) <= 16 * 2.0 ** -24 * s + 2.0 ** -126).all(), gap
+
+
+@pytest.mark.parametrize("E,T", KERNELS)
+def test_sigmoid_weights_of_very_negative_logits(E, T):
+    """Scores below the least normal number: their shares are those of exp(z), and by themselves they are zero."""
+    rng = np.random.default_rng(E)
+    lost = np.zeros(E, dtype=np.uint8)
+    for at in (-20.0, -40.0, -86.0, -95.0, -110.0, -1e4):
+        logits = rng.standard_normal((T, E)) + at
+        logits[:, 7] = -np.inf
+        w, z, s = weights(E, T, 6, "sigmoid", logits, lost, True, seed=E)
+        e = np.exp(z - z.max(axis=1, keepdims=True)) / (1 + np.exp(z))
+        want = e / e.sum(axis=1, keepdims=True)
+        assert (np.abs(w - want) <= 16 * 2.0 ** -24 * want).all(), at
+        w, z, s = weights(E, T, 6, "sigmoid", logits, lost, False, seed=E)
+        assert (np.abs(w - s) <= 16 * 2.0 ** -24 * s + 2.0 ** -126).all(), at
+
+
+@pytest.mark.parametrize("score_fn", ["softmax", "sigmoid"])
+def test_weights_of_nothing_but_minus_infinity(score_fn):
+    """0 / 0 renormalised, as in the gate without a bias; zero otherwise."""
+    for T in (4, 3001):
+        logits = np.zeros((T, 64))
+        lost = np.zeros(64, dtype=np.uint8)
+        bias = np.random.default_rng(0).permutation(64)
+        logits[:, np.argsort(-bias)[:6]] = -np.inf  # the chosen ones
+        w, _, _ = weights(64, T, 6, score_fn, logits, lost, True)
+        assert np.isnan(w).all()
+        w, _, _ = weights(64, T, 6, score_fn, logits, lost, False)
+        assert (w == 0).all()
