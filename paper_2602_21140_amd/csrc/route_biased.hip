@@ -119,16 +119,22 @@ __device__ __forceinline__ float exp_below(float z, float m) {
   const float d = z - m, t = d - z, more = (z - (d - t)) - (m + t);
   return d < -100.f ? exp_of(-100.f, 0.f) : exp_of(d, more);
 }
-// Softmax scores of the chosen experts, `shift` and `scale` being those of the row.  Renormalised, what a score shares with the
-// others goes out, and it is taken from the largest chosen logit, `top`: a larger one that is lost, or kept back by the bias,
-// would leave nothing but zeros of scores 87 below it.  A row whose scores are NaN has `scale` NaN.
-__device__ __forceinline__ float softmax_chosen(float z, float top, float shift, float scale, bool renormalise) {
-  return exp_below(z, renormalise ? top : shift) * scale;
-}
-// Sigmoid scores.  Below -30 a score is exp(z) to all bits of fp32; where all chosen ones are, they are renormalised as above.
-__device__ __forceinline__ float sigmoid_chosen(float z, float top, bool renormalise) {
-  if (z < -30.f) return exp_below(z, renormalise && top < -30.f ? top : 0.f);
-  return __builtin_amdgcn_rcpf(1.0f + exp_of(z > 87.f ? -87.f : -z, 0.f));
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_of(z > 87.f ? -87.f : -z, 0.f)); }
+
+// Scores of the chosen experts of a token, which LANES lanes have, `mine` of them an expert; `shift` and `scale` are those of its
+// softmax.  Where a score is too small for fp32, those of a renormalised token keep their shares: they are taken from the largest
+// chosen logit, and what they have in common goes out.  (The token's largest may be lost, or kept back by the bias, and would
+// leave nothing but zeros of scores 87 below it.  Below -30 a sigmoid is exp(z) to all bits of fp32.)  A token whose scores are
+// NaN has `scale` NaN.  Hardly a call has such a score, and a wavefront without one passes that over.
+template <int LANES>
+__device__ __forceinline__ float chosen_score(float z, float shift, float scale, bool sig, bool renormalise, bool mine) {
+  const float s = sig ? sigmoid(z) : exp_below(z, shift) * scale;
+  const unsigned long long small = __ballot(mine && z - (sig ? 0.f : shift) < (sig ? -30.f : -80.f));
+  if (small == 0) return s;
+  const float top = LANES == 16 ? row_max(mine ? z : kOut) : wave_max(mine ? z : kOut);
+  if (sig) return z < -30.f ? exp_below(z, renormalise && top < -30.f ? top : 0.f) : s;
+  const bool here = LANES == 16 ? (small >> (threadIdx.x & 48) & 0xFFFFull) != 0 : true;
+  return renormalise && here ? exp_below(z, top) * scale : s;
 }
 
 __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j, int e, float weight) {
@@ -269,8 +275,7 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
     }
     my_e = min(my_e, p.E - 1);
     const float zc = z[my_e];
-    const float top = row_max(li < p.k ? zc : kOut);
-    const float sc = sig ? sigmoid_chosen(zc, top, p.renormalise) : softmax_chosen(zc, top, shift, scale, p.renormalise);
+    const float sc = chosen_score<16>(zc, shift, scale, sig, p.renormalise, li < p.k);
     const float total = p.renormalise ? row_sum(li < p.k ? sc : 0.f) : 1.f;
     if (li < p.k && t < p.T) store_choice(p, t, li, my_e, sc / total * p.route_scale);
   }
@@ -396,8 +401,7 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   }
 
   const float zc = z[my_e];
-  const float top = wave_max(lane < p.k ? zc : kOut);
-  const float sc = sig ? sigmoid_chosen(zc, top, p.renormalise) : softmax_chosen(zc, top, shift, scale, p.renormalise);
+  const float sc = chosen_score<64>(zc, shift, scale, sig, p.renormalise, lane < p.k);
   const float sum = p.renormalise ? wave_sum(lane < p.k ? sc : 0.f) : 1.f;
   if (lane < p.k) store_choice(p, t, lane, my_e, sc / sum * p.route_scale);
 }
