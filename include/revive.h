@@ -248,15 +248,19 @@ int revive_route(revive_ctx* ctx, const void* x, const void* w_router, float* lo
  *   scores     softmax over all E logits (lost experts' included), or elementwise
  *              sigmoid, in fp32.  The order of the keys is that of fp32 numbers:
  *              keys closer than their rounding may swap.
- *   n_group > 1: a group scores the sum of its two best keys above -inf, in fp32.
+ *   n_group > 1: a group scores the sum of its two best keys above -inf, rounded
+ *              as an fp32 number whose range it cannot leave.
  *   topk_weight: the chosen expert's score (without the bias); renormalise != 0:
  *              over the sum of the chosen scores, as exact where these are too
  *              small for fp32 (a row of nothing but scores of logits -inf: 0 / 0,
  *              NaN); otherwise a score below 2^-126 is 0.  Then times route_scale.
  * A key that is NaN or -inf orders nothing: its expert counts as absent while
- * live experts with other keys are left, in its group's score too, and is chosen
- * after them, in ascending id (the weight of a NaN score is NaN; renormalised, so
- * are its row's).  Bias may be infinite: +inf puts an expert in front of all others.
+ * live experts of kept groups with other keys are left, in its group's score too,
+ * and is chosen after them, in ascending id; groups of nothing but such keys come
+ * after the others (the weight of a NaN score is NaN; renormalised, so are its
+ * row's).  Every other bias counts: masked by the lowest fp32 number an expert is
+ * the last of the numbers; +inf puts it in front of all others, unless its score is
+ * NaN, and so its key.
  * Everything else (mask, ties, replicas, token offset) is revive_route's. */
 int revive_route_biased(revive_ctx* ctx, const void* x, const void* w_router, float* logits,
                         int32_t logits_given, const float* bias, int32_t renormalise, int32_t T,

@@ -5,8 +5,9 @@
 //   a group's score is the sum of its two best keys above -inf (the one, if there is one); the topk_group best groups are kept
 //   top-k by key, ties to the lower id;  weight_j = s_{e_j} [/ sum_j s_{e_j}] * route_scale
 //
-// All of it in fp32.  What is no number has a place among the keys: NaN and -inf are kNone or less, behind every number and alike
-// but for their ids; an expert that is lost, taken or in a dropped group is -inf.
+// All of it in fp32.  What is no number has a place among the keys: NaN and -inf are kNone, behind every number and alike but for
+// their ids; an expert that is lost, taken or in a dropped group is -inf.  kNone is fp32's lowest number, and keys that are numbers
+// begin at the one above it, which a bias of the lowest number counts as.
 #include "ctx.hpp"
 
 namespace revive {
@@ -26,18 +27,22 @@ struct BiasedParams {
   float route_scale;
 };
 
-constexpr float kNone = -1e38f;
+constexpr float kNone = -0x1.fffffep127f, kLowest = -0x1.fffffcp127f;
 constexpr float kOut = -__builtin_inff();
 
-// Bias of an expert, made so that the sum with a score (kNone if it is NaN) is the key.
+// Bias of an expert as key_of wants it: -inf without a live replica, kNone for a NaN or -inf, else a number from kLowest up or +inf.
+__device__ __forceinline__ float bias_of(float b, int count) {
+  const float number = b == kNone ? kLowest : b, place = fmaxf(number, kNone);
+  return count > 0 ? place : kOut;
+}
 __device__ __forceinline__ float bias_of(const BiasedParams& p, int e, bool is) {
   e = min(e, p.E - 1);
-  const float b = p.bias[e];
-  const int count = p.l2p_count[e];
-  return is && count > 0 ? fmaxf(b, kNone) : kOut;
+  return bias_of(p.bias[e], is ? p.l2p_count[e] : 0);
 }
-// Score of a group from its two best keys.
-__device__ __forceinline__ float group_score(float m1, float m2) { return m2 < 0.5f * kNone ? m1 : m1 + m2; }
+// Scores are NaN or in [0, 1], so that a sum is no less than its bias; fmaxf passes a NaN over.
+__device__ __forceinline__ float key_of(float score, float bias) { return fmaxf(score + bias, fminf(bias, kNone)); }
+// Half the score of a group (which fp32 always holds) from its two best keys; kNone and -inf of groups without a number.
+__device__ __forceinline__ float group_score(float m1, float m2) { return m2 > kNone ? fmaf(0.5f, m1, 0.5f * m2) : m1 > kNone ? 0.5f * m1 : m1; }
 
 // Cross-lane steps as operands of an ALU instruction: 0 to 3 combine lanes 1, 2, 4 and 8 apart inside rows of 16, after which
 // every lane of a row has the row's result; 4 and 5 bring the rows' results to lanes 31 and 63, and then to lane 63; 6 and 7
@@ -174,10 +179,10 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
       const int e = c * 4 < n ? expert(c * 4) : 0;  // n is a multiple of 4
       const f32x4 b = *reinterpret_cast<const f32x4*>(p.bias + e);
       const int4 k = *reinterpret_cast<const int4*>(p.l2p_count + e);
-      bias[c * 4] = c * 4 < n && k.x > 0 ? fmaxf(b[0], kNone) : kOut;
-      bias[c * 4 + 1] = c * 4 < n && k.y > 0 ? fmaxf(b[1], kNone) : kOut;
-      bias[c * 4 + 2] = c * 4 < n && k.z > 0 ? fmaxf(b[2], kNone) : kOut;
-      bias[c * 4 + 3] = c * 4 < n && k.w > 0 ? fmaxf(b[3], kNone) : kOut;
+      bias[c * 4] = bias_of(b[0], c * 4 < n ? k.x : 0);
+      bias[c * 4 + 1] = bias_of(b[1], c * 4 < n ? k.y : 0);
+      bias[c * 4 + 2] = bias_of(b[2], c * 4 < n ? k.z : 0);
+      bias[c * 4 + 3] = bias_of(b[3], c * 4 < n ? k.w : 0);
     }
   } else {
 #pragma unroll
@@ -217,7 +222,7 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
       for (int i = 0; i < V; ++i) s[i >> 2][i & 3] *= scale;
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) s[i >> 2][i & 3] = fmaxf(s[i >> 2][i & 3], kNone) + bias[i];
+    for (int i = 0; i < V; ++i) s[i >> 2][i & 3] = key_of(s[i >> 2][i & 3], bias[i]);
     if (GROUPED) {
       float m1 = kOut, m2 = kOut;
 #pragma unroll
@@ -313,7 +318,7 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
     for (int i = 0; i < V; ++i) key[i] *= scale;
   }
 #pragma unroll
-  for (int i = 0; i < V; ++i) key[i] = fmaxf(key[i], kNone) + bias[i];
+  for (int i = 0; i < V; ++i) key[i] = key_of(key[i], bias[i]);
 
   if (p.n_group > 1) {
     const int gsz = p.E / p.n_group;
