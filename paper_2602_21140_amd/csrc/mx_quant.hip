@@ -95,18 +95,37 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(QuantArgs a) {
   }
 }
 
+// A grid has fewer than 2^32 threads in x (a launch of more runs what is left of them modulo 2^32, without an error): rows that
+// one launch can take.
+constexpr int64_t kMaxThreads = (1ll << 32) - 256;
+int64_t rows_of_launch(int row_threads_log2) { return kMaxThreads >> row_threads_log2; }
+dim3 grid_of(int64_t rows, int units, int row_threads_log2) {
+  return dim3(static_cast<uint32_t>(((rows << row_threads_log2) + 255) / 256), ceil_div(units, kUnits << row_threads_log2));
+}
+int row_threads_log2_of(int units) {
+  int n = 2;
+  while (n < 8 && (kUnits << n) < units) ++n;
+  return n;
+}
+
 template <typename El, bool TILED>
 int launch_quantize(const QuantArgs& base, hipStream_t stream, const revive_ctx* ctx) {
   QuantArgs a = base;
-  if (a.rows == 0 || a.units == 0) return REVIVE_OK;
-  a.row_threads_log2 = 2;
-  while (a.row_threads_log2 < 8 && (kUnits << a.row_threads_log2) < a.units) ++a.row_threads_log2;
-  const int64_t gx = (a.rows * (1 << a.row_threads_log2) + 255) / 256;
-  if (gx > 0x7fffffff) return fail(ctx, REVIVE_EINVAL, "mx quantize: too many rows");
-  const dim3 grid(static_cast<uint32_t>(gx), ceil_div(a.units, kUnits << a.row_threads_log2));
-  if (a.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes) hipLaunchKernelGGL((mx_quantize_kernel<El, true, TILED>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((mx_quantize_kernel<El, false, TILED>), grid, dim3(256), 0, stream, a);
-  return check_hip(ctx, hipGetLastError(), "mx_quantize launch");
+  if (a.units == 0) return REVIVE_OK;
+  a.row_threads_log2 = row_threads_log2_of(a.units);
+  const bool once = base.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes;
+  for (int64_t row = 0; row < base.rows; row += a.rows) {
+    a.rows = std::min(base.rows - row, rows_of_launch(a.row_threads_log2));
+    a.x = static_cast<const El*>(base.x) + row * a.ld;
+    a.codes = base.codes + row * a.code_row;
+    a.scales = base.scales + row * a.scale_row;
+    const dim3 grid = grid_of(a.rows, a.units, a.row_threads_log2);
+    if (once) hipLaunchKernelGGL((mx_quantize_kernel<El, true, TILED>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((mx_quantize_kernel<El, false, TILED>), grid, dim3(256), 0, stream, a);
+    const int rc = check_hip(ctx, hipGetLastError(), "mx_quantize launch");
+    if (rc != REVIVE_OK) return rc;
+  }
+  return REVIVE_OK;
 }
 
 struct DequantArgs {
@@ -165,14 +184,20 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(DequantArgs a) {
 template <typename El>
 int launch_dequantize(const DequantArgs& base, hipStream_t stream) {
   DequantArgs a = base;
-  a.row_threads_log2 = 2;
-  while (a.row_threads_log2 < 8 && (kUnits << a.row_threads_log2) < a.units) ++a.row_threads_log2;
-  const int64_t gx = (a.rows * (1 << a.row_threads_log2) + 255) / 256;
-  if (gx > 0x7fffffff) return fail(nullptr, REVIVE_EINVAL, "revive_mx_dequantize: too many rows");
-  const dim3 grid(static_cast<uint32_t>(gx), ceil_div(a.units, kUnits << a.row_threads_log2));
-  if (a.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes) hipLaunchKernelGGL((mx_dequantize_kernel<El, true>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((mx_dequantize_kernel<El, false>), grid, dim3(256), 0, stream, a);
-  return check_hip(nullptr, hipGetLastError(), "mx_dequantize launch");
+  a.row_threads_log2 = row_threads_log2_of(a.units);
+  const bool once = base.rows * a.K * static_cast<int64_t>(sizeof(El)) > kOnceBytes;
+  for (int64_t row = 0; row < base.rows; row += a.rows) {
+    a.rows = std::min(base.rows - row, rows_of_launch(a.row_threads_log2));
+    a.codes = base.codes + row * a.blocks * 16;
+    a.scales = base.scales + row * a.blocks;
+    a.out = static_cast<El*>(base.out) + row * a.ld;
+    const dim3 grid = grid_of(a.rows, a.units, a.row_threads_log2);
+    if (once) hipLaunchKernelGGL((mx_dequantize_kernel<El, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((mx_dequantize_kernel<El, false>), grid, dim3(256), 0, stream, a);
+    const int rc = check_hip(nullptr, hipGetLastError(), "mx_dequantize launch");
+    if (rc != REVIVE_OK) return rc;
+  }
+  return REVIVE_OK;
 }
 
 // Rows of codes and scales into the packed layout: a thread moves the 16 bytes of a lane, or a lane's word of scales.  Done
