@@ -116,9 +116,11 @@ int revive_create(const revive_config* cfg /*host*/, revive_ctx** out);
 int revive_destroy(revive_ctx* ctx);
 
 /* Size of the scratch workspace the data-path calls need (block histograms,
- * GEMM tile lists, the FFN's intermediate activations), and binding of a
- * caller-owned device buffer of at least that size (256-byte aligned).  The
- * buffer must stay valid until the context is destroyed or another is bound.
+ * GEMM tile lists, the FFNs' intermediate activations), and binding of a
+ * caller-owned device buffer of at least that size (256-byte aligned).  A buffer
+ * may be smaller where revive_mx_expert_ffn, which keeps its activations in it too,
+ * needs more than the other calls do: those run in it, and that one is refused
+ * (REVIVE_ENOMEM).  The buffer must stay valid until the context is destroyed or another is bound.
  * Binding writes a few bytes of the buffer (synchronously); the data-path
  * calls of one context share the workspace, so calls that overlap in time on
  * different streams race. */

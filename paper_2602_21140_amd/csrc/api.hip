@@ -114,7 +114,7 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
   off = align_up(off + ctx->elem * N_max * c.I, 256);
   w.off_h_shared = off;
   off = align_up(off + ctx->elem * static_cast<size_t>(c.T_max) * c.I_shared, 256);
-  w.bytes = off;
+  w.bytes = w.mx_bytes = off;
   if (c.dtype == REVIVE_DTYPE_BF16) {
     off = w.off_h;
     auto codes_and_scales = [&off](int64_t rows, int K, size_t& codes, size_t& scales) {
@@ -126,7 +126,7 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
     codes_and_scales(c.T_max, c.H, w.off_mx_x, w.off_mx_x_scales);
     codes_and_scales(N_max, c.I, w.off_mx_h, w.off_mx_h_scales);
     codes_and_scales(c.T_max, c.I_shared, w.off_mx_h_shared, w.off_mx_h_shared_scales);
-    w.bytes = std::max(w.bytes, off);
+    w.mx_bytes = std::max(w.bytes, off);
   }
 
   int rc = check_hip(nullptr, hipGetDevice(&ctx->device), "hipGetDevice");
@@ -169,7 +169,7 @@ int revive_destroy(revive_ctx* ctx) {
 
 int revive_workspace_bytes(const revive_ctx* ctx, size_t* bytes) {
   if (!ctx || !bytes) return fail(ctx, REVIVE_EINVAL, "revive_workspace_bytes: null argument");
-  *bytes = ctx->ws.bytes;
+  *bytes = ctx->ws.mx_bytes;
   return REVIVE_OK;
 }
 
@@ -317,6 +317,8 @@ int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
   int rc = check_call(ctx, "revive_mx_expert_ffn", T, true);
   if (rc != REVIVE_OK) return rc;
   if (ctx->cfg.dtype != REVIVE_DTYPE_BF16) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: the layer must be bf16");
+  if (ctx->ws_bound < ctx->ws.mx_bytes)
+    return fail(ctx, REVIVE_ENOMEM, "revive_mx_expert_ffn: a workspace of %zu bytes is bound, %zu needed", ctx->ws_bound, ctx->ws.mx_bytes);
   if (T == 0) return REVIVE_OK;
   if (!x || !src_of || !slot_offsets || !w_gate_up || !w_down || !y_perm) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: null argument");
   if (y_shared) {

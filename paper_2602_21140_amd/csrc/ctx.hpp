@@ -72,7 +72,8 @@ struct Workspace {
   size_t off_mx_x, off_mx_x_scales;                // x: codes [T_max][mx_code_row(H)], scales [T_max][mx_scale_row(H)]
   size_t off_mx_h, off_mx_h_scales;                // h: codes (mx_h_at), scales [N_max][mx_scale_row(I)]
   size_t off_mx_h_shared, off_mx_h_shared_scales;  // the shared expert's h
-  size_t bytes;
+  size_t bytes;           // what every call but the 4-bit FFN needs
+  size_t mx_bytes;        // what that one needs, and so all of them
 };
 
 struct TimingSlot {
