@@ -470,6 +470,8 @@ class ReviveLayer:
         for w, n in [(w, n_gu) for w in w_gate_up] + [(w, n_dn) for w in w_down]:
             if w is not None:
                 assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.data_ptr() % 16 == 0
+        I_shared = self.cfg.I_shared
+        self._mx_shared_bytes = (2 * mx_packed_bytes(I_shared, self.cfg.H), mx_packed_bytes(self.cfg.H, I_shared)) if I_shared else None
         self._mx_keep = (list(w_gate_up), list(w_down))
         self._mx_tabs = tuple(torch.tensor([0 if w is None else w.data_ptr() for w in ws], dtype=torch.int64).to(self.device)
                               for ws in (w_gate_up, w_down))
@@ -543,17 +545,34 @@ class ReviveLayer:
 
     def mx_expert_ffn(self, x, src_of, slot_offsets, T: int, w_sh_gate_up=None, w_sh_down=None, out=None, stream=None):
         """revive_mx_expert_ffn: (y_perm, y_shared) of the 4-bit experts; x [T, H] as it came, rows found through src_of."""
+        # Checks in three expressions and addresses without _ptr: of the 10.1 us of the smallest call the checks are 1.3.
         assert self._mx_tabs is not None, "set_mx_expert_weights first"
-        if x.dtype is not torch.bfloat16 or not x.is_contiguous():
-            raise ValueError("x: contiguous rows of bfloat16 expected")
-        use_shared = w_sh_gate_up is not None
+        N, H = T * self.cfg.k, self.cfg.H
+        if (x.dtype is not torch.bfloat16 or x.shape[-1] != H or x.numel() < T * H or not x.is_contiguous() or not x.is_cuda
+                or src_of.dtype is not torch.int32 or src_of.numel() < N or not src_of.is_contiguous() or not src_of.is_cuda
+                or slot_offsets.dtype is not torch.int32 or slot_offsets.numel() <= self.P or not slot_offsets.is_contiguous() or not slot_offsets.is_cuda):
+            raise ValueError(f"x {x.dtype} {tuple(x.shape)}, src_of {src_of.dtype} {tuple(src_of.shape)}, slot_offsets {slot_offsets.dtype} "
+                             f"{tuple(slot_offsets.shape)}: contiguous bfloat16 {(T, H)} and int32 {N} and {self.P + 1} in device memory expected")
+        gate_up = down = shared = None
+        if w_sh_gate_up is not None:
+            n = self._mx_shared_bytes  # None: no shared expert
+            if (n is None or w_sh_down is None or w_sh_gate_up.dtype is not torch.uint8 or w_sh_gate_up.numel() != n[0] or not w_sh_gate_up.is_contiguous()
+                    or not w_sh_gate_up.is_cuda or w_sh_down.dtype is not torch.uint8 or w_sh_down.numel() != n[1] or not w_sh_down.is_contiguous()
+                    or not w_sh_down.is_cuda):
+                raise ValueError(f"the shared expert's weights: {'none' if n is None else n} contiguous bytes of gate and up, and of down, in device memory expected")
+            gate_up, down = w_sh_gate_up.data_ptr(), w_sh_down.data_ptr()
         if out is None:
-            out = (self.empty(T * self.cfg.k, self.cfg.H), self.empty(T, self.cfg.H) if use_shared else None)
+            out = (self.empty(N, H), self.empty(T, H) if gate_up is not None else None)
         y_perm, y_shared = out
-        self._check(self.L.revive_mx_expert_ffn(self._ctx, _ptr(x), _ptr(src_of), _ptr(slot_offsets), _ptr(self._mx_tabs[0]),
-                                                _ptr(self._mx_tabs[1]), _ptr(y_perm), _ptr(w_sh_gate_up) if use_shared else None,
-                                                _ptr(w_sh_down) if use_shared else None, _ptr(y_shared) if use_shared else None, T,
-                                                self._stream(stream)))
+        if y_perm.dtype is not torch.bfloat16 or y_perm.numel() < N * H or not y_perm.is_contiguous() or not y_perm.is_cuda:
+            raise ValueError(f"y_perm {y_perm.dtype} {tuple(y_perm.shape)}: contiguous bfloat16 {(N, H)} in device memory expected")
+        if gate_up is not None:
+            if y_shared is None or y_shared.dtype is not torch.bfloat16 or y_shared.numel() < T * H or not y_shared.is_contiguous() or not y_shared.is_cuda:
+                raise ValueError(f"y_shared: contiguous bfloat16 {(T, H)} in device memory expected, the shared expert's weights are given")
+            shared = y_shared.data_ptr()
+        tabs = self._mx_tabs
+        self._check(self.L.revive_mx_expert_ffn(self._ctx, x.data_ptr(), src_of.data_ptr(), slot_offsets.data_ptr(), tabs[0].data_ptr(), tabs[1].data_ptr(),
+                                                y_perm.data_ptr(), gate_up, down, shared, T, _current_stream(stream)))
         return y_perm, y_shared
 
     def shared_ffn(self, x, w_sh_gate_up, w_sh_down, T: int, out=None, stream=None):
