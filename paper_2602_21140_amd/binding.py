@@ -491,17 +491,19 @@ class ReviveLayer:
 
     def route_biased(self, x, w_router, bias, T: int, renormalise=True, logits=None, logits_given=False, out=None, stream=None):
         """revive_route_biased: experts chosen by score + bias (fp32 [E]), weighted by the score."""
-        k = self.cfg.k
-        if bias.dtype is not torch.float32 or bias.numel() != self.cfg.E or not bias.is_contiguous() or not bias.is_cuda:
-            raise ValueError(f"bias: {self.cfg.E} contiguous float32 in device memory expected")
+        k, E = self.cfg.k, self.cfg.E
+        if bias.dtype is not torch.float32 or bias.numel() != E or not bias.is_contiguous() or not bias.is_cuda:
+            raise ValueError(f"bias: {E} contiguous float32 in device memory expected")
         if logits is None:
-            logits = self.empty(T, self.cfg.E, dtype=torch.float32)
+            logits = self.empty(T, E, dtype=torch.float32)
         if out is None:
             out = (self.empty(T, k, dtype=torch.int32), self.empty(T, k, dtype=torch.float32),
                    self.empty(T, k, dtype=torch.int32))
         top_l, top_w, top_p = out
-        self._check(self.L.revive_route_biased(self._ctx, _ptr(x), _ptr(w_router), _ptr(logits), int(bool(logits_given)), _ptr(bias),
-                                               int(bool(renormalise)), T, _ptr(top_l), _ptr(top_w), _ptr(top_p), self._stream(stream)))
+        if logits.dtype is not torch.float32 or logits.numel() < T * E or not logits.is_contiguous() or not logits.is_cuda:
+            raise ValueError(f"logits {logits.dtype} {tuple(logits.shape)}: contiguous float32 {(T, E)} in device memory expected")
+        self._check(self.L.revive_route_biased(self._ctx, _ptr(x), _ptr(w_router), logits.data_ptr(), 1 if logits_given else 0, bias.data_ptr(),
+                                               1 if renormalise else 0, T, top_l.data_ptr(), top_w.data_ptr(), top_p.data_ptr(), _current_stream(stream)))
         return logits, top_l, top_w, top_p
 
     def dispatch_index(self, topk_phys, T: int, out=None, stream=None):
@@ -510,6 +512,8 @@ class ReviveLayer:
         if out is None:
             out = (self.empty(self.P + 1, dtype=torch.int32), self.empty(N, dtype=torch.int32), self.empty(N, dtype=torch.int32))
         slot_offsets, dst_row, src_of = out
+        if N and (topk_phys.dtype is not torch.int32 or topk_phys.numel() < N or not topk_phys.is_contiguous() or not topk_phys.is_cuda):
+            raise ValueError(f"topk_phys {topk_phys.dtype} {tuple(topk_phys.shape)}: contiguous int32 {(T, self.cfg.k)} in device memory expected")
         self._check(self.L.revive_dispatch_index(self._ctx, _ptr(topk_phys), T, _ptr(slot_offsets), _ptr(dst_row), _ptr(src_of),
                                                  self._stream(stream)))
         return slot_offsets, dst_row, src_of
