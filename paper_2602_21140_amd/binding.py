@@ -324,8 +324,8 @@ def mx_pack(codes: torch.Tensor, scales: torch.Tensor, out=None, stream=None) ->
     n = mx_packed_bytes(rows, K)
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=codes.device)
-    if out.dtype != torch.uint8 or out.numel() != n or not out.is_contiguous():
-        raise ValueError(f"out: {n} contiguous bytes expected")
+    if out.dtype != torch.uint8 or out.numel() != n or not out.is_contiguous() or not out.is_cuda:
+        raise ValueError(f"out: {n} contiguous bytes in device memory expected")
     _check_free(lib().revive_mx_pack(codes.data_ptr(), scales.data_ptr(), rows, K, out.data_ptr(), _current_stream(stream)))
     return out
 
@@ -469,7 +469,8 @@ class ReviveLayer:
         n_gu, n_dn = 2 * mx_packed_bytes(self.cfg.I, self.cfg.H), mx_packed_bytes(self.cfg.H, self.cfg.I)
         for w, n in [(w, n_gu) for w in w_gate_up] + [(w, n_dn) for w in w_down]:
             if w is not None:
-                assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.data_ptr() % 16 == 0
+                assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.is_cuda and w.data_ptr() % 16 == 0
+        assert all((a is None) == (b is None) for a, b in zip(w_gate_up, w_down)), "a slot has both of its matrices or none"
         I_shared = self.cfg.I_shared
         self._mx_shared_bytes = (2 * mx_packed_bytes(I_shared, self.cfg.H), mx_packed_bytes(self.cfg.H, I_shared)) if I_shared else None
         self._mx_keep = (list(w_gate_up), list(w_down))
