@@ -147,6 +147,9 @@ class MicrobatchPipeline:
         cfg = base.cfg
         if n_micro < 1 or cfg.T % n_micro:
             raise ValueError("T must be a multiple of the number of microbatches")
+        for p in np.nonzero(base.p2l >= 0)[0]:
+            if base.gu[p] is None or base.dn[p] is None:
+                raise ValueError(f"slot {p} holds an expert without bf16 or fp32 weights, which the microbatches multiply by")
         self.base, self.n, self.Tm = base, n_micro, cfg.T // n_micro
         Tm, k, H, E, P = self.Tm, cfg.k, cfg.H, cfg.E, cfg.P
         i32, f32 = torch.int32, torch.float32
