@@ -43,18 +43,35 @@ class ResidentMxLayer(ResidentLayer):
         if sh is not None:
             self.buf["y_shared"] = L.empty(T, cfg.H)
 
-    def forward(self, logits: Optional[torch.Tensor] = None, stream=None, **_kw) -> Dict[str, Optional[torch.Tensor]]:
+    def forward(self, logits: Optional[torch.Tensor] = None, shared=True, stream=None, overlap_shared=True,
+                stage_marks: Optional[list] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """As ResidentLayer.forward, in 4-bit form.  The shared expert is served by the launches of the routed ones, so that
+        overlap_shared, which would put it on a stream beside them, changes nothing here."""
         L, b, T = self.layer, self.buf, self.cfg.T
         main = torch.cuda.current_stream() if stream is None else stream
         given = logits is not None
+        sh = self.mx_sh if shared else (None, None)
+        y_shared = b["y_shared"] if sh[0] is not None else None
+
+        def mark():
+            if stage_marks is not None:
+                ev = torch.cuda.Event(enable_timing=True)
+                ev.record(main)
+                stage_marks.append(ev)
+
+        mark()
         if given:
             with torch.cuda.stream(main):
                 b["logits"].copy_(logits)
         L.route_biased(None if given else self.x, None if given else self.w_router_packed, self.bias, T, logits=b["logits"],
                        logits_given=given, out=(b["topk_logical"], b["topk_weight"], b["topk_phys"]), stream=main)
+        mark()
         L.dispatch_index(b["topk_phys"], T, out=(b["slot_offsets"], b["dst_row"], b["src_of"]), stream=main)
-        L.mx_expert_ffn(self.x, b["src_of"], b["slot_offsets"], T, *self.mx_sh, out=(b["y_perm"], b["y_shared"]), stream=main)
-        L.combine(b["y_perm"], b["dst_row"], b["topk_weight"], b["y_shared"], T, out=b["out"], stream=main)
+        mark()
+        L.mx_expert_ffn(self.x, b["src_of"], b["slot_offsets"], T, *sh, out=(b["y_perm"], y_shared), stream=main)
+        mark()
+        L.combine(b["y_perm"], b["dst_row"], b["topk_weight"], y_shared, T, out=b["out"], stream=main)
+        mark()
         return b
 
 
