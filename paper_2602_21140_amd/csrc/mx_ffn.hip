@@ -22,13 +22,15 @@ constexpr int kMxCus = 256;
 // 215, 16 tokens 373 and 357 to 377.  Of more tokens a slot may have several row-tiles, which a launch of some microseconds
 // outweighs where there is little to stream in all: 40 slots of 1024 x 512, 32 tokens 13.1 and 14.8, 64 13.1 and 16.8, 128 14.5 and
 // 16.0; 72 of 2048 x 1408, 32 tokens 53 and 57, 64 61 and 64, 128 66 and 64; 128 of 4096 x 256, 64 tokens 47 and 52; but 288 of
-// 7168 x 2048 (6 GB), 32 tokens 620 and 588, 64 863 and 866.
+// 7168 x 2048 (6 GB), 32 tokens 620 and 588, 64 863 and 866.  (So the launch is as good or up to 4 % better from 8 to 16 tokens of
+// the largest layers, which the line, drawn for the others, gives away.)
 constexpr int kMxFewTokens = 16, kMxFewTokensSmall = 64;
 constexpr int64_t kMxSmallBytes = 1ll << 30;
 // Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below
 // it the streaming kernel, which starts sooner.  us, streaming and tiles: 288 slots, H = 7168, I = 2048: 14 rows 1146 and 1192,
 // 28 rows 1276 and 1242, 57 rows 1426 and 1329; 72 slots, H = 2048, I = 1408: 21 rows 73 and 75, 43 rows 83 and 82; 40 slots, H =
 // 1024, I = 512: 26 rows 18 and 22, 102 rows 26 and 24; 128 slots, H = 4096, I = 256: 8 rows 57 and 61, 32 rows 79 and 72.
+// The host knows no row counts: the average is over all slots, without rows or not, so that a load on few slots crosses later.
 constexpr int kMxTileRowsPerSlot = 32;
 
 struct MxFfn {

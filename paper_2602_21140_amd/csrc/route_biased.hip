@@ -157,8 +157,10 @@ __device__ __forceinline__ void store_choice(const BiasedParams& p, int t, int j
 // holds n = ceil(E / 16) <= V of its experts, dealt so that the run's loads are contiguous: lane j of the run holds the group's
 // experts j, j + lg, ..., or with WIDE (E a multiple of 64, 16-byte loads) its words of four j, j + lg, ...
 //
-// Bound by the ALU: 8192 tokens of 256 experts in 8 groups, k = 8, 7.7 us (1.2 TB/s), 32 768 of 384 experts 21.2 (2.5 TB/s); with a
-// wavefront per token 12.9 and 36.  What a choice costs is kept small by two levels: a lane has the best key of every four of its experts in
+// Bound by the ALU where there are many tokens: 32 768 of 384 experts, k = 8, 20.8 us (2.5 TB/s), with vector instructions in 72 % of
+// the cycles in which a CU is busy.  8192 of 256 experts in 8 groups 7.9 us (1.2 TB/s), 43 %: two wavefronts a SIMD, which wait for
+// their loads and then for one choice after the other.  With a wavefront per token 33.1 and 12.6.  What a choice costs is kept
+// small by two levels: a lane has the best key of every four of its experts in
 // registers and the keys in LDS; a round looks at the bests, and the four keys of the winning one are read, stripped of the
 // winner and put back.
 template <int V, bool GROUPED, bool WIDE>
@@ -287,7 +289,8 @@ __global__ __launch_bounds__(256) void route_biased_rows_kernel(BiasedParams p, 
 }
 
 // A wavefront per token; lane l holds experts l, l + 64, ...  Bound by latency: the choices follow one another, each a maximum over
-// the wavefront.  64 tokens of 256 experts in 8 groups, k = 8, 6.0 us; 512 of 512 experts, k = 16, 8.1.
+// the wavefront (vector instructions in 20 % of the cycles).  64 tokens of 256 experts in 8 groups, k = 8, 5.8 us; 512 of 512
+// experts, k = 16, 7.6.
 template <int V>
 __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
   const int lane = threadIdx.x & 63;
@@ -415,13 +418,13 @@ __global__ __launch_bounds__(256) void route_biased_kernel(BiasedParams p) {
 
 // Which kernel.  A row of lanes per token does a quarter of the work, but one after the other: it wins once a wavefront per token
 // keeps the ALUs busy, later where experts are no multiple of 64 and its loads are of four bytes.  us in a graph, a row and a
-// wavefront per token: 256 experts in 8 groups, k = 8, 1024 tokens 6.7 and 6.2, 2048 6.8 and 6.9, 3000 6.8 and 7.9, 8192 7.9 and
-// 12.9; 384, k = 8, 2048 6.6 and 6.1, 3000 6.7 and 6.6, 8192 7.7 and 9.9; 512, k = 16, 2048 10.7 and 9.2, 3000 10.8 and 10.4, 4096
-// 10.9 and 11.7; 64, k = 2, 3000 3.2 and 3.0, 4096 3.2 and 3.4; 100, k = 4, 4096 5.0 and 4.1, 8192 5.4 and 5.1; 500, k = 8, 6144
-// 13.0 and 11.0, 8192 13.2 and 13.1.
+// wavefront per token: 256 experts in 8 groups, k = 8, 1024 tokens 6.8 and 6.0, 2048 6.9 and 6.6, 3000 6.9 and 7.3, 8192 7.9 and
+// 12.6; 384, k = 8, 2048 6.8 and 5.8, 3000 6.9 and 6.4, 8192 7.8 and 10.2; 512, k = 16, 2048 10.9 and 8.4, 3000 11.1 and 9.9, 4096
+// 11.2 and 11.3; 64, k = 2, 3000 3.3 and 3.3, 4096 3.4 and 3.6; 100, k = 4, 4096 4.9 and 4.3, 8192 5.4 and 5.6; 500, k = 8, 6144
+// 13.2 and 10.0, 8192 13.3 and 13.0.
 constexpr int kRowsFrom = 3000, kNarrowRowsFrom = 8192;
-// Workgroups of the rows' kernel at most; beyond them each takes its share of tokens.  32768 tokens, 384 experts: 512 26.7, 1024
-// 21.4, 2048 22.2.
+// Workgroups of the rows' kernel at most; beyond them each takes its share of tokens.  32768 tokens of 384 experts: 512 26.6, 1024
+// 20.6, 2048 20.5; of 256 in 8 groups 24.7, 18.7 and 18.6.
 constexpr int kRowsWorkgroups = 1024;
 
 int launch_route_biased(revive_ctx* ctx, const float* logits, const float* bias, bool renormalise, int T, int32_t* topk_logical,
