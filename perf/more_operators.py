@@ -39,8 +39,8 @@ def _quantize(name, rows, K, dtype):
     return dict(name=name, op="quantize", rows=rows, K=K, dtype=dtype)
 
 
-def _linear(name, rows, K, N, bias=False, activation="none", residual=False, dtype="bf16"):
-    return dict(name=name, op="linear", rows=rows, K=K, N=N, bias=bias, activation=activation, residual=residual, dtype=dtype)
+def _linear(name, rows, K, N, bias=False, activation="none", residual=False):
+    return dict(name=name, op="linear", rows=rows, K=K, N=N, bias=bias, activation=activation, residual=residual)
 
 
 def _ffn(name, shape, T, k, n_failed=1, skew=0.0, **changes):
@@ -63,8 +63,8 @@ def listed():
         _linear("linear_one_token", 1, 7168, 7168, residual=True),
         # the same of a decode batch
         _linear("linear_decode", 64, 7168, 7168, residual=True),
-        # a ragged chunk, an odd number of columns, everything in the epilogue, fp32 results
-        _linear("linear_odd", 1003, 2048, 1411, bias=True, activation="gelu", residual=True, dtype="fp32"),
+        # a ragged chunk, an odd number of columns, everything in the epilogue
+        _linear("linear_odd", 1003, 2048, 1411, bias=True, activation="gelu", residual=True),
         # a prefill chunk
         _linear("linear_prefill", 8192, 7168, 7168, bias=True, residual=True),
         # a decode batch: two rows per expert, nearly every expert's weights are streamed once
@@ -94,7 +94,7 @@ def draw(rng):
         while True:
             c = dict(op=op, rows=_log_int(rng, 1, 8192), K=32 * _log_int(rng, 1, 512), N=_log_int(rng, 1, 16384),
                      bias=rng.random() < 0.5, activation=rng.choice(["none", "none", "relu", "silu", "gelu"]),
-                     residual=rng.random() < 0.5, dtype=rng.choice(["bf16", "bf16", "fp32"]))
+                     residual=rng.random() < 0.5)
             if c["rows"] * c["K"] * c["N"] <= 8192 * 7168 * 7168 and c["K"] * c["N"] <= 16384 * 7168:
                 return c
     while True:
@@ -141,7 +141,7 @@ def _linear_inputs(c, seed):
     x = _codes(_normal(gen, c.rows, c.K) * torch.exp(0.5 * _normal(gen, c.rows, 1)))
     w = _codes(_normal(gen, c.N, c.K) * c.K ** -0.5)
     bias = 0.5 * _normal(gen, c.N) if c.bias else None
-    residual = (3 * _normal(gen, c.rows, c.N)).to(DTYPES[c.dtype]) if c.residual else None
+    residual = (3 * _normal(gen, c.rows, c.N)).to(torch.bfloat16) if c.residual else None
     return x, w, bias, residual
 
 
@@ -246,7 +246,7 @@ def _prepare_linear(c, seed):
         from paper_2602_21140_amd import binding
         s.lib = binding
         s.w = binding.mx8_pack(*s.w)
-        s.out = torch.empty(c.rows, c.N, dtype=DTYPES[c.dtype], device=DEVICE)
+        s.out = torch.empty(c.rows, c.N, dtype=torch.bfloat16, device=DEVICE)
     return s
 
 
@@ -314,7 +314,7 @@ def _plain_linear(s):
     z = _activated(z, s.c.activation)
     if s.residual is not None:
         z = z + s.residual.float()
-    return {"out": z.to(DTYPES[s.c.dtype])}
+    return {"out": z.to(torch.bfloat16)}
 
 
 def _plain_swiglu(x, gate_up, down):
@@ -375,8 +375,7 @@ def work(case):
         b = 2 if c.dtype == "bf16" else 4
         return {"bytes": int(c.rows * c.K * (2 * b + 33 / 32)), "flops": 4 * c.rows * c.K}
     if c.op == "linear":
-        b = 2 if c.dtype == "bf16" else 4
-        return {"bytes": int((c.rows + c.N) * c.K * 33 / 32 + c.rows * c.N * b * (2 if c.residual else 1)), "flops": 2 * c.rows * c.K * c.N}
+        return {"bytes": int((c.rows + c.N) * c.K * 33 / 32 + c.rows * c.N * (4 if c.residual else 2)), "flops": 2 * c.rows * c.K * c.N}
     live, N = (c.n_ranks - c.n_failed) * c.slots_per_rank, c.T * c.k
     used = live * (1 - (1 - c.k / live) ** c.T)
     weights = 3 * c.H * (used * c.I + c.I_shared) * 33 / 32
