@@ -83,6 +83,7 @@ typedef enum revive_status {
 
 enum { REVIVE_SCORE_SOFTMAX = 0, REVIVE_SCORE_SIGMOID = 1 };
 enum { REVIVE_DTYPE_F32 = 0, REVIVE_DTYPE_BF16 = 1 };
+enum { REVIVE_ACT_NONE = 0, REVIVE_ACT_RELU = 1, REVIVE_ACT_SILU = 2, REVIVE_ACT_GELU = 3 };
 
 typedef struct revive_config {
   int32_t T_max;          /* largest token count of any call                     */
@@ -120,7 +121,8 @@ int revive_destroy(revive_ctx* ctx);
  * caller-owned device buffer of at least that size (256-byte aligned).  A buffer
  * may be smaller where revive_mx_expert_ffn, which keeps its activations in it too,
  * needs more than the other calls do: those run in it, and that one is refused
- * (REVIVE_ENOMEM).  The buffer must stay valid until the context is destroyed or another is bound.
+ * (REVIVE_ENOMEM); so with revive_mx_eight_expert_ffn.  The buffer must stay valid until
+ * the context is destroyed or another is bound.
  * Binding writes a few bytes of the buffer (synchronously); the data-path
  * calls of one context share the workspace, so calls that overlap in time on
  * different streams race. */
@@ -391,6 +393,105 @@ int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
                          const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int32_t T,
                          revive_stream stream);
 
+/* ---- microscaled 8-bit floats (MXFP8) -------------------------------------
+ *
+ * As the 4-bit ones, with a byte a number ("eight" in the calls' names, which are of
+ * letters alone): a block of 32 numbers along K has a
+ * scale 2^e, kept as the byte e + 127, and its numbers are kept as E4M3 codes
+ * (sign, 4 bits of exponent, 3 of mantissa; the largest is 448).
+ *   e = the smallest with largest magnitude <= 448 * 2^e, at least -127; zeros: byte 0
+ *   code = x / 2^e rounded to the nearest, ties to the even code
+ * A block that holds an infinity or a NaN gets byte 255 and stands for 32 NaNs.
+ * The calls that take no context launch on `stream` of the current device, allocate
+ * nothing and may be captured.  Their errors: revive_last_error(NULL).
+ *
+ * revive_mx_eight_quantize:
+ *   x       dev [rows, K], fp32 or bf16 (dtype), rows ld elements apart
+ *   codes   dev uint8 [rows, 32 * ceil(K/32)], 16-byte aligned; the last block filled
+ *           up with zeros
+ *   scales  dev uint8 [rows, ceil(K/32)]
+ * revive_mx_eight_dequantize: the numbers they stand for, [rows, K], rows ld elements apart;
+ *   fp32 holds them exactly, bf16 those of 2^-133 and above (others are rounded to it).
+ * K <= 2^24.  Rows may start at any address that fits their elements. */
+int revive_mx_eight_quantize(const void* x, int32_t dtype, int64_t rows, int32_t K, int64_t ld, uint8_t* codes,
+                        uint8_t* scales, revive_stream stream);
+int revive_mx_eight_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t K, int32_t dtype,
+                          void* out, int64_t ld, revive_stream stream);
+
+/* Weights of the 8-bit products: codes and scales of an output-major matrix [rows, K]
+ * (K a multiple of 32, rows * K < 2^32) into the order in which the kernels read them.
+ * revive_mx_eight_packed_bytes gives the size of `packed` (dev, 16-byte aligned).  Rows
+ * are filled up with zeros to a multiple of 128, K to one of 128.  Packed, a matrix is
+ *   codes  [rows/128][K/128][8][2][64][16 bytes]: blocks of 16 rows x 128 K; lane
+ *          l = 0..63 of a block's half h has K 64*h + 16*(l/16) .. +15 of its row l%16
+ *   scales [rows/128][K/128][64][8 bytes]: byte b of lane l is the scale of block b's
+ *          row l%16 and K 32*(l/16) .. +31
+ * and row m of block b (0..7) of a panel is the matrix' row 32*(b/2) + 8*(m/4) +
+ * 4*(b%2) + m%4 of the panel.  A gate and an up matrix follow each other. */
+int revive_mx_eight_packed_bytes(int32_t rows, int32_t K, size_t* bytes /*host*/);
+int revive_mx_eight_pack(const uint8_t* codes, const uint8_t* scales, int32_t rows, int32_t K, void* packed,
+                    revive_stream stream);
+
+/* Norm in front of the layer, with the residual's addition and an 8-bit output:
+ *   s = x + residual                       rounded to dtype
+ *   y = s / sqrt(mean(s^2) + eps) * weight rounded to dtype; the mean over a row, in fp64
+ *   codes, scales = what revive_mx_eight_quantize makes of y
+ *   x          dev [rows, H] dtype (fp32 or bf16), rows ld_x elements apart
+ *   residual   dev [rows, H] dtype, rows ld_residual elements apart; NULL: s = x
+ *   weight     dev [H] dtype
+ *   sum        dev [rows, H] dtype: s; NULL: not wanted (always without a residual)
+ *   y          dev [rows, H] dtype; NULL: only the 8-bit form is wanted
+ *   codes, scales  as of revive_mx_eight_quantize; both NULL: not wanted
+ * H <= 2^24, eps finite and not negative (with 0, a row of zeros gives NaN).  Rows may
+ * start at any address that fits their elements.  sum or y may be x or residual itself
+ * (rows H elements apart), but not one buffer; otherwise nothing overlaps.  No context; launches on
+ * `stream` of the current device, allocates nothing, may be captured.  Errors:
+ * revive_last_error(NULL). */
+int revive_add_rms_norm(const void* x, const void* residual /*nullable*/, const void* weight, int32_t dtype, int64_t rows,
+                        int32_t H, int64_t ld_x, int64_t ld_residual, float eps, void* sum /*nullable*/, void* y /*nullable*/,
+                        uint8_t* codes /*nullable*/, uint8_t* scales /*nullable*/, revive_stream stream);
+
+/* Matrix product with bias, activation and residual in its epilogue, on 8-bit
+ * activations and weights:  out = act(x W^T + bias) + residual, fp32 sums (with what the
+ * note below says), one rounding to bf16.
+ *   x, x_scales  dev: codes [rows, K], 16-byte aligned, and scales [rows, K/32]; K a
+ *                multiple of 32 (a row of another length comes filled up with zeros)
+ *   w            dev: packed [N, K] (revive_mx_eight_pack), N * K < 2^32
+ *   bias         dev fp32 [N]; NULL: none
+ *   activation   REVIVE_ACT_*: none, max(z, 0), z / (1 + exp(-z)), z times the normal
+ *                distribution's function
+ *   residual     dev [rows, N] bf16, rows ld_residual elements apart; NULL: none
+ *   out          dev [rows, N] bf16, rows ld_out elements apart.  May be the residual
+ *                itself, with the same distance of rows; otherwise nothing overlaps.
+ * The matrix cores add up 8-bit products in groups of 8 consecutive K, each cut off at
+ * 2^-13 of the power of two of the group's largest; groups and sums are added in fp32.
+ * Results are off by some 2^-15 of their size so: less than bf16 resolves.
+ * Deterministic: a row's results do not depend on the other rows' contents.  No context;
+ * launches on `stream` of the current device, allocates nothing, may be captured.
+ * Errors: revive_last_error(NULL). */
+int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales, int32_t rows, int32_t K, const void* w, int32_t N,
+                      const float* bias /*nullable*/, int32_t activation, const void* residual /*nullable*/,
+                      int64_t ld_residual, void* out, int64_t ld_out, revive_stream stream);
+
+/* Expert FFN on microscaled 8-bit weights and activations, for bf16 layers.  With Q the
+ * rounding above along a row, for every slot p with rows [slot_offsets[p],
+ * slot_offsets[p+1]):  h = Q(silu(x G_p) * (x U_p)),  y = h D_p, sums as of the product
+ * above, and the same on all T rows of x for the shared expert when y_shared != NULL.
+ *   x, x_scales  dev: the tokens' codes [T, H], 16-byte aligned, and scales [T, H/32], not
+ *              permuted (revive_add_rms_norm, revive_mx_eight_quantize)
+ *   src_of     dev int32 [N] (revive_dispatch_index): row r is token src_of[r] / k
+ *   w_gate_up  dev table of P dev pointers: packed gate matrix [I, H] followed by
+ *              the packed up matrix;  w_down: packed [H, I].  Entries of slots that
+ *              receive no rows are never dereferenced.
+ *   y_perm     dev [N, H] bf16;  rows beyond slot_offsets[P] are left alone
+ *   w_sh_gate_up, w_sh_down, y_shared [T, H]: shared expert, may be NULL
+ * Outputs and weights are 16-byte aligned.  Uses the whole workspace: not to overlap
+ * with another FFN call of the same context. */
+int revive_mx_eight_expert_ffn(revive_ctx* ctx, const uint8_t* x, const uint8_t* x_scales, const int32_t* src_of,
+                          const int32_t* slot_offsets, const void* const* w_gate_up, const void* const* w_down,
+                          void* y_perm, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int32_t T,
+                          revive_stream stream);
+
 /* a9 - Combine / E2A (Sec. 2.3): out[t, :] = sum_j topk_weight[t, j] *
  * y_perm[dst_row[t*k + j], :] (+ y_shared[t, :]); fp32 accumulation in
  * ascending j, shared expert last, one rounding to dtype.
@@ -429,6 +530,8 @@ enum {
   REVIVE_K_MX_QUANTIZE,
   REVIVE_K_MX_GATE_UP,
   REVIVE_K_MX_DOWN,
+  REVIVE_K_MX8_GATE_UP,
+  REVIVE_K_MX8_DOWN,
   REVIVE_K_COUNT
 };
 

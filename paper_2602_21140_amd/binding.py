@@ -24,7 +24,8 @@ TORCH_DTYPE = {"fp32": torch.float32, "bf16": torch.bfloat16}
 
 KERNEL_NAMES = ["router_gemm", "route_topk", "dispatch_index",
                 "dispatch_permute", "ffn_tiles", "ffn_gate_up", "ffn_down", "ffn_shared_gate_up",
-                "ffn_shared_down", "combine", "expert_counts", "mx_quantize", "mx_gate_up", "mx_down"]
+                "ffn_shared_down", "combine", "expert_counts", "mx_quantize", "mx_gate_up", "mx_down",
+                "mx8_gate_up", "mx8_down"]
 
 
 class ReviveError(RuntimeError):
@@ -86,6 +87,13 @@ def lib() -> C.CDLL:
         "revive_mx_packed_bytes": (C.c_int, [i32, i32, P(sz)]),
         "revive_mx_pack": (C.c_int, [vp, vp, i32, i32, vp, vp]),
         "revive_mx_expert_ffn": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
+        "revive_mx_eight_quantize": (C.c_int, [vp, i32, C.c_int64, i32, C.c_int64, vp, vp, vp]),
+        "revive_mx_eight_dequantize": (C.c_int, [vp, vp, C.c_int64, i32, i32, vp, C.c_int64, vp]),
+        "revive_mx_eight_packed_bytes": (C.c_int, [i32, i32, P(sz)]),
+        "revive_mx_eight_pack": (C.c_int, [vp, vp, i32, i32, vp, vp]),
+        "revive_add_rms_norm": (C.c_int, [vp, vp, vp, i32, C.c_int64, i32, C.c_int64, C.c_int64, C.c_float, vp, vp, vp, vp, vp]),
+        "revive_mx_eight_linear": (C.c_int, [vp, vp, i32, i32, vp, i32, vp, i32, vp, C.c_int64, vp, C.c_int64, vp]),
+        "revive_mx_eight_expert_ffn": (C.c_int, [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
         "revive_dispatch": (C.c_int, [vp, vp, vp, i32, vp, vp, vp, vp, vp]),
         "revive_set_token_offset": (C.c_int, [vp, C.c_int64]),
         "revive_get_rank_map": (C.c_int, [vp, vp, vp]),
@@ -120,6 +128,8 @@ EXPORTS = ["revive_create", "revive_destroy", "revive_workspace_bytes", "revive_
            "revive_get_rank_map", "revive_rank_offsets", "revive_set_token_offset",
            "revive_route_biased", "revive_dispatch_index", "revive_mx_quantize", "revive_mx_dequantize", "revive_mx_packed_bytes",
            "revive_mx_pack", "revive_mx_expert_ffn",
+           "revive_mx_eight_quantize", "revive_mx_eight_dequantize", "revive_mx_eight_packed_bytes", "revive_mx_eight_pack", "revive_add_rms_norm",
+           "revive_mx_eight_linear", "revive_mx_eight_expert_ffn",
            "revive_route", "revive_dispatch", "revive_dispatch_static", "revive_expert_ffn", "revive_shared_ffn", "revive_combine",
            "revive_graph_begin", "revive_graph_end", "revive_graph_launch", "revive_graph_exec_id",
            "revive_graph_destroy", "revive_set_kernel_timing", "revive_kernel_time",
@@ -337,6 +347,160 @@ def mx_pack_expert(gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> 
     return torch.cat([g, u]), d
 
 
+# ---- microscaled 8-bit floats, the norm that gives them and the product that takes them ------------
+
+ACTIVATION = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def _here(stream, *tensors):
+    """All of them (None aside) are in the memory of the current device, on which a call without a context launches."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{tuple(t.shape)} {t.dtype}: in device memory expected")
+        if device is None:
+            device = torch.cuda.current_device()
+        if t.get_device() != device:
+            raise ValueError(f"{tuple(t.shape)} {t.dtype} is on {t.device}, the current device is {device}")
+    if stream is not None and device is not None and stream.device_index != device:
+        raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")
+
+
+def _mx8_check_form(codes: torch.Tensor, scales: torch.Tensor, rows: int, n: int):
+    """codes [rows, 32 n] and scales [rows, n], contiguous uint8."""
+    if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or codes.shape != (rows, 32 * n) or scales.shape != (rows, n)
+            or not codes.is_contiguous() or not scales.is_contiguous()):
+        raise ValueError(f"codes {codes.dtype} {tuple(codes.shape)} and scales {scales.dtype} {tuple(scales.shape)}: contiguous uint8 "
+                         f"{(rows, 32 * n)} and {(rows, n)} expected")
+
+
+def _mx8_form(rows: int, n: int, device) -> Tuple[torch.Tensor, torch.Tensor]:
+    return (torch.empty(rows, 32 * n, dtype=torch.uint8, device=device), torch.empty(rows, n, dtype=torch.uint8, device=device))
+
+
+def mx8_quantize(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """revive_mx_eight_quantize: x [rows, K] fp32 or bf16 (rows may be strided) -> (codes [rows, 32 n], scales [rows, n]), n =
+    ceil(K / 32) blocks of 32."""
+    dtype, rows, K, ld = _mx_rows(x, "x")
+    n = (K + MX_BLOCK - 1) // MX_BLOCK
+    codes, scales = _mx8_form(rows, n, x.device) if out is None else out
+    _mx8_check_form(codes, scales, rows, n)
+    _here(stream, x, codes, scales)
+    _check_free(lib().revive_mx_eight_quantize(x.data_ptr(), dtype, rows, K, ld, codes.data_ptr(), scales.data_ptr(), _current_stream(stream)))
+    return codes, scales
+
+
+def mx8_dequantize(codes: torch.Tensor, scales: torch.Tensor, K: Optional[int] = None, dtype=torch.bfloat16, out=None,
+                   stream=None) -> torch.Tensor:
+    """revive_mx_eight_dequantize: the numbers that codes and scales stand for, [rows, K] (default: all of the blocks, or out's)."""
+    if out is None:
+        rows, n = scales.shape
+        out = torch.empty(rows, MX_BLOCK * n if K is None else K, dtype=dtype, device=codes.device)
+    code, rows, width, ld = _mx_rows(out, "out")
+    if K is not None and width != K:
+        raise ValueError(f"out {tuple(out.shape)}: {K} columns expected")
+    _mx8_check_form(codes, scales, rows, (width + MX_BLOCK - 1) // MX_BLOCK)
+    _here(stream, codes, scales, out)
+    _check_free(lib().revive_mx_eight_dequantize(codes.data_ptr(), scales.data_ptr(), rows, width, code, out.data_ptr(), ld, _current_stream(stream)))
+    return out
+
+
+def mx8_packed_bytes(rows: int, K: int) -> int:
+    n = C.c_size_t()
+    _check_free(lib().revive_mx_eight_packed_bytes(rows, K, C.byref(n)))
+    return n.value
+
+
+def mx8_pack(codes: torch.Tensor, scales: torch.Tensor, out=None, stream=None) -> torch.Tensor:
+    """revive_mx_eight_pack: an output-major weight matrix' codes and scales -> uint8 in the order that the 8-bit products read."""
+    if scales.dim() != 2:
+        raise ValueError("codes and scales are matrices")
+    rows, K = scales.shape[0], scales.shape[1] * MX_BLOCK
+    _mx8_check_form(codes, scales, rows, scales.shape[1])
+    n = mx8_packed_bytes(rows, K)
+    if out is None:
+        out = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    if out.dtype != torch.uint8 or out.numel() != n or not out.is_contiguous():
+        raise ValueError(f"out: {n} contiguous bytes expected")
+    _here(stream, codes, scales, out)
+    _check_free(lib().revive_mx_eight_pack(codes.data_ptr(), scales.data_ptr(), rows, K, out.data_ptr(), _current_stream(stream)))
+    return out
+
+
+def mx8_pack_expert(gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Math-layout expert matrices (gate/up [H, I], down [I, H], fp32 or bf16) -> (w_gate_up, w_down), quantised along each
+    product's K and packed."""
+    g, u, d = (mx8_pack(*mx8_quantize(w.t().contiguous())) for w in (gate, up, down))
+    return torch.cat([g, u]), d
+
+
+def _dense(t: Optional[torch.Tensor], what: str, shape, dtype):
+    if t is not None and (t.dtype is not dtype or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{what} {t.dtype} {tuple(t.shape)}: contiguous {dtype} {tuple(shape)} expected")
+
+
+def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, quantize=False,
+                 out=None, stream=None):
+    """revive_add_rms_norm: (sum, y, codes, scales) of x [rows, H] (rows of x and of the residual may be strided).
+
+    sum is None without a residual, codes and scales without `quantize`.  out: the four to be written, None for each that is not
+    wanted (codes and scales together; with `quantize` they are); sum or y may be x or the residual."""
+    dtype, rows, H, ld = _mx_rows(x, "x")
+    ld_r = H
+    if residual is not None:
+        if residual.dtype is not x.dtype or residual.shape != x.shape:
+            raise ValueError(f"residual {residual.dtype} {tuple(residual.shape)}: {x.dtype} {tuple(x.shape)} expected")
+        ld_r = _mx_rows(residual, "residual")[3]
+    _dense(weight, "weight", (H,), x.dtype)
+    n = (H + MX_BLOCK - 1) // MX_BLOCK
+    if out is None:
+        empty = lambda: torch.empty(rows, H, dtype=x.dtype, device=x.device)  # noqa: E731
+        out = (None if residual is None else empty(), empty(), *(_mx8_form(rows, n, x.device) if quantize else (None, None)))
+    total, y, codes, scales = out
+    _dense(total, "sum", (rows, H), x.dtype)
+    _dense(y, "y", (rows, H), x.dtype)
+    if (codes is None) != (not quantize) or (scales is None) != (not quantize):
+        raise ValueError("codes and scales are given exactly where quantize is true")
+    if quantize:
+        _mx8_check_form(codes, scales, rows, n)
+    _here(stream, x, weight, residual, total, y, codes, scales)
+    _check_free(lib().revive_add_rms_norm(x.data_ptr(), _ptr(residual), weight.data_ptr(), dtype, rows, H, ld, ld_r, eps, _ptr(total), _ptr(y),
+                                          _ptr(codes), _ptr(scales), _current_stream(stream)))
+    return out
+
+
+def mx8_linear(codes: torch.Tensor, scales: torch.Tensor, w: torch.Tensor, n_out: int, bias: Optional[torch.Tensor] = None,
+               activation: str = "none", residual: Optional[torch.Tensor] = None, out=None, stream=None) -> torch.Tensor:
+    """revive_mx_eight_linear: act(x W^T + bias) + residual [rows, n_out] bf16 of x's codes and scales and mx8_pack's w.
+
+    Rows of out and of the residual may be strided; out may be the residual."""
+    if scales.dim() != 2 or activation not in ACTIVATION:
+        raise ValueError(f"codes and scales are matrices, and the activation one of {sorted(ACTIVATION)}: {activation!r}")
+    rows, n = scales.shape
+    K = MX_BLOCK * n
+    _mx8_check_form(codes, scales, rows, n)
+    n_bytes = mx8_packed_bytes(n_out, K)
+    if w.dtype is not torch.uint8 or w.numel() != n_bytes or not w.is_contiguous():
+        raise ValueError(f"w {w.dtype} {tuple(w.shape)}: {n_bytes} contiguous bytes of mx8_pack expected")
+    _dense(bias, "bias", (n_out,), torch.float32)
+    if out is None:
+        out = torch.empty(rows, n_out, dtype=torch.bfloat16, device=codes.device)
+    _, out_rows, width, ld = _mx_rows(out, "out")
+    if (out_rows, width) != (rows, n_out) or out.dtype is not torch.bfloat16:
+        raise ValueError(f"out {out.dtype} {tuple(out.shape)}: bfloat16 {(rows, n_out)} expected")
+    ld_r = n_out
+    if residual is not None:
+        if residual.dtype is not out.dtype or residual.shape != out.shape:
+            raise ValueError(f"residual {residual.dtype} {tuple(residual.shape)}: {out.dtype} {tuple(out.shape)} expected")
+        ld_r = _mx_rows(residual, "residual")[3]
+    _here(stream, codes, scales, w, bias, residual, out)
+    _check_free(lib().revive_mx_eight_linear(codes.data_ptr(), scales.data_ptr(), rows, K, w.data_ptr(), n_out, _ptr(bias), ACTIVATION[activation],
+                                        _ptr(residual), ld_r, out.data_ptr(), ld, _current_stream(stream)))
+    return out
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -364,6 +528,7 @@ class ReviveLayer:
             self._check(self.L.revive_bind_workspace(self._ctx, self.workspace.data_ptr(), self.workspace.numel()))
         self._w_tabs = None
         self._mx_tabs = None
+        self._mx8_tabs = None
         self._graphs: List[C.c_void_p] = []
 
     # -- plumbing --------------------------------------------------------------------------
@@ -477,6 +642,20 @@ class ReviveLayer:
         self._mx_tabs = tuple(torch.tensor([0 if w is None else w.data_ptr() for w in ws], dtype=torch.int64).to(self.device)
                               for ws in (w_gate_up, w_down))
 
+    def set_mx8_expert_weights(self, w_gate_up: Sequence[Optional[torch.Tensor]], w_down: Sequence[Optional[torch.Tensor]]):
+        """Per-slot packed 8-bit weights (mx8_pack_expert; lists of P tensors, None for empty slots) -> device pointer tables."""
+        assert len(w_gate_up) == self.P and len(w_down) == self.P
+        n_gu, n_dn = 2 * mx8_packed_bytes(self.cfg.I, self.cfg.H), mx8_packed_bytes(self.cfg.H, self.cfg.I)
+        for w, n in [(w, n_gu) for w in w_gate_up] + [(w, n_dn) for w in w_down]:
+            if w is not None:
+                assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.is_cuda and w.data_ptr() % 16 == 0
+        assert all((a is None) == (b is None) for a, b in zip(w_gate_up, w_down)), "a slot has both of its matrices or none"
+        I_shared = self.cfg.I_shared
+        self._mx8_shared_bytes = (2 * mx8_packed_bytes(I_shared, self.cfg.H), mx8_packed_bytes(self.cfg.H, I_shared)) if I_shared else None
+        self._mx8_keep = (list(w_gate_up), list(w_down))
+        self._mx8_tabs = tuple(torch.tensor([0 if w is None else w.data_ptr() for w in ws], dtype=torch.int64).to(self.device)
+                              for ws in (w_gate_up, w_down))
+
     # -- data path -------------------------------------------------------------------------
     def route(self, x, w_router, T: int, logits=None, logits_given=False, out=None, stream=None):
         k = self.cfg.k
@@ -578,6 +757,46 @@ class ReviveLayer:
         tabs = self._mx_tabs
         self._check(self.L.revive_mx_expert_ffn(self._ctx, x.data_ptr(), src_of.data_ptr(), slot_offsets.data_ptr(), tabs[0].data_ptr(), tabs[1].data_ptr(),
                                                 y_perm.data_ptr(), gate_up, down, shared, T, _current_stream(stream)))
+        return y_perm, y_shared
+
+    def mx8_expert_ffn(self, codes, scales, src_of, slot_offsets, T: int, w_sh_gate_up=None, w_sh_down=None, out=None, stream=None):
+        """revive_mx_eight_expert_ffn: (y_perm, y_shared) of the 8-bit experts; x's codes [T, H] and scales [T, H / 32] as they came, rows
+        found through src_of."""
+        assert self._mx8_tabs is not None, "set_mx8_expert_weights first"
+        N, H = T * self.cfg.k, self.cfg.H
+        if (codes.dtype is not torch.uint8 or codes.shape[-1] != H or codes.numel() < T * H or not codes.is_contiguous() or not codes.is_cuda
+                or scales.dtype is not torch.uint8 or scales.shape[-1] != H // MX_BLOCK or scales.numel() < T * (H // MX_BLOCK)
+                or not scales.is_contiguous() or not scales.is_cuda):
+            raise ValueError(f"codes {codes.dtype} {tuple(codes.shape)} and scales {scales.dtype} {tuple(scales.shape)}: contiguous uint8 "
+                             f"{(T, H)} and {(T, H // MX_BLOCK)} in device memory expected")
+        if (src_of.dtype is not torch.int32 or src_of.numel() < N or not src_of.is_contiguous() or not src_of.is_cuda
+                or slot_offsets.dtype is not torch.int32 or slot_offsets.numel() <= self.P or not slot_offsets.is_contiguous() or not slot_offsets.is_cuda):
+            raise ValueError(f"src_of {src_of.dtype} {tuple(src_of.shape)}, slot_offsets {slot_offsets.dtype} {tuple(slot_offsets.shape)}: "
+                             f"contiguous int32 {N} and {self.P + 1} in device memory expected")
+        gate_up = down = shared = None
+        if (w_sh_gate_up is None) != (w_sh_down is None):
+            raise ValueError("the shared expert's weights come together")
+        if w_sh_gate_up is not None:
+            n = self._mx8_shared_bytes  # None: no shared expert
+            if (n is None or w_sh_gate_up.dtype is not torch.uint8 or w_sh_gate_up.numel() != n[0] or not w_sh_gate_up.is_contiguous()
+                    or not w_sh_gate_up.is_cuda or w_sh_down.dtype is not torch.uint8 or w_sh_down.numel() != n[1] or not w_sh_down.is_contiguous()
+                    or not w_sh_down.is_cuda):
+                raise ValueError(f"the shared expert's weights: {'none' if n is None else n} contiguous bytes of gate and up, and of down, in device memory expected")
+            gate_up, down = w_sh_gate_up.data_ptr(), w_sh_down.data_ptr()
+        if out is None:
+            out = (self.empty(N, H), self.empty(T, H) if gate_up is not None else None)
+        y_perm, y_shared = out
+        if y_perm.dtype is not torch.bfloat16 or y_perm.numel() < N * H or not y_perm.is_contiguous() or not y_perm.is_cuda:
+            raise ValueError(f"y_perm {y_perm.dtype} {tuple(y_perm.shape)}: contiguous bfloat16 {(N, H)} in device memory expected")
+        if gate_up is not None:
+            if y_shared is None or y_shared.dtype is not torch.bfloat16 or y_shared.numel() < T * H or not y_shared.is_contiguous() or not y_shared.is_cuda:
+                raise ValueError(f"y_shared: contiguous bfloat16 {(T, H)} in device memory expected, the shared expert's weights are given")
+            shared = y_shared.data_ptr()
+        _here(stream, codes, scales, src_of, slot_offsets, w_sh_gate_up, w_sh_down, y_perm)
+        tabs = self._mx8_tabs
+        self._check(self.L.revive_mx_eight_expert_ffn(self._ctx, codes.data_ptr(), scales.data_ptr(), src_of.data_ptr(), slot_offsets.data_ptr(),
+                                                 tabs[0].data_ptr(), tabs[1].data_ptr(), y_perm.data_ptr(), gate_up, down, shared, T,
+                                                 _current_stream(stream)))
         return y_perm, y_shared
 
     def shared_ffn(self, x, w_sh_gate_up, w_sh_down, T: int, out=None, stream=None):

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "librevive.so")
 SOURCES = ["api.hip", "map_host.cpp", "route.hip", "dispatch.hip", "ffn.hip", "combine.hip", "study.hip",
-           "route_biased.hip", "mx_quant.hip", "mx_ffn.hip"]
+           "route_biased.hip", "mx_quant.hip", "mx_ffn.hip", "mx8_quant.hip", "mx8_linear.hip", "mx8_ffn.hip", "norm.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

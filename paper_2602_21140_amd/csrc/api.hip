@@ -6,6 +6,7 @@
 
 #include "ctx.hpp"
 #include "mx.hpp"
+#include "mx8.hpp"
 
 namespace revive {
 
@@ -114,7 +115,7 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
   off = align_up(off + ctx->elem * N_max * c.I, 256);
   w.off_h_shared = off;
   off = align_up(off + ctx->elem * static_cast<size_t>(c.T_max) * c.I_shared, 256);
-  w.bytes = w.mx_bytes = off;
+  w.bytes = w.mx_bytes = w.mx8_bytes = off;
   if (c.dtype == REVIVE_DTYPE_BF16) {
     off = w.off_h;
     auto codes_and_scales = [&off](int64_t rows, int K, size_t& codes, size_t& scales) {
@@ -127,6 +128,16 @@ int revive_create(const revive_config* cfg, revive_ctx** out) {
     codes_and_scales(N_max, c.I, w.off_mx_h, w.off_mx_h_scales);
     codes_and_scales(c.T_max, c.I_shared, w.off_mx_h_shared, w.off_mx_h_shared_scales);
     w.mx_bytes = std::max(w.bytes, off);
+    off = w.off_h;
+    auto mx8_form = [&off](int64_t rows, int K, size_t& codes, size_t& scales) {
+      codes = off;
+      off = align_up(off + static_cast<size_t>(rows) * K, 256);
+      scales = off;
+      off = align_up(off + static_cast<size_t>(rows) * (K / kMx8Block), 256);
+    };
+    mx8_form(N_max, c.I, w.off_mx8_h, w.off_mx8_h_scales);
+    mx8_form(c.T_max, c.I_shared, w.off_mx8_h_shared, w.off_mx8_h_shared_scales);
+    w.mx8_bytes = std::max(w.bytes, off);
   }
 
   int rc = check_hip(nullptr, hipGetDevice(&ctx->device), "hipGetDevice");
@@ -169,7 +180,7 @@ int revive_destroy(revive_ctx* ctx) {
 
 int revive_workspace_bytes(const revive_ctx* ctx, size_t* bytes) {
   if (!ctx || !bytes) return fail(ctx, REVIVE_EINVAL, "revive_workspace_bytes: null argument");
-  *bytes = ctx->ws.mx_bytes;
+  *bytes = std::max(ctx->ws.mx_bytes, ctx->ws.mx8_bytes);
   return REVIVE_OK;
 }
 
@@ -330,6 +341,27 @@ int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
   if (reinterpret_cast<uintptr_t>(x) % 2 != 0) return fail(ctx, REVIVE_EINVAL, "revive_mx_expert_ffn: x is not aligned to its elements");
   return launch_mx_expert_ffn(ctx, x, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T,
                               static_cast<hipStream_t>(stream));
+}
+
+int revive_mx_eight_expert_ffn(revive_ctx* ctx, const uint8_t* x, const uint8_t* x_scales, const int32_t* src_of, const int32_t* slot_offsets,
+                          const void* const* w_gate_up, const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down,
+                          void* y_shared, int32_t T, revive_stream stream) {
+  const char* who = "revive_mx_eight_expert_ffn";
+  int rc = check_call(ctx, who, T, true);
+  if (rc != REVIVE_OK) return rc;
+  if (ctx->cfg.dtype != REVIVE_DTYPE_BF16) return fail(ctx, REVIVE_EINVAL, "%s: the layer must be bf16", who);
+  if (ctx->ws_bound < ctx->ws.mx8_bytes)
+    return fail(ctx, REVIVE_ENOMEM, "%s: a workspace of %zu bytes is bound, %zu needed", who, ctx->ws_bound, ctx->ws.mx8_bytes);
+  if (T == 0) return REVIVE_OK;
+  if (!x || !x_scales || !src_of || !slot_offsets || !w_gate_up || !w_down || !y_perm) return fail(ctx, REVIVE_EINVAL, "%s: null argument", who);
+  if (y_shared) {
+    if (ctx->cfg.I_shared == 0) return fail(ctx, REVIVE_EINVAL, "%s: y_shared given but the layer has no shared expert", who);
+    if (!w_sh_gate_up || !w_sh_down) return fail(ctx, REVIVE_EINVAL, "%s: the shared expert needs both weight matrices", who);
+  }
+  for (const void* p : {static_cast<const void*>(x), static_cast<const void*>(y_perm), static_cast<const void*>(y_shared), w_sh_gate_up, w_sh_down})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return fail(ctx, REVIVE_EINVAL, "%s: codes, outputs and weights must be 16-byte aligned", who);
+  return launch_mx8_expert_ffn(ctx, x, x_scales, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T,
+                               static_cast<hipStream_t>(stream));
 }
 
 int revive_dispatch(revive_ctx* ctx, const void* x, const int32_t* topk_phys, int32_t T, void* x_perm,
@@ -498,7 +530,7 @@ const char* revive_kernel_name(int32_t kernel) {
   static const char* names[REVIVE_K_COUNT] = {
       "router_gemm", "route_topk", "dispatch_index", "dispatch_permute",
       "ffn_tiles", "ffn_gate_up", "ffn_down", "ffn_shared_gate_up", "ffn_shared_down", "combine", "expert_counts",
-      "mx_quantize", "mx_gate_up", "mx_down"};
+      "mx_quantize", "mx_gate_up", "mx_down", "mx8_gate_up", "mx8_down"};
   return kernel >= 0 && kernel < REVIVE_K_COUNT ? names[kernel] : "?";
 }
 

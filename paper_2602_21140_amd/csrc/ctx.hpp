@@ -72,8 +72,12 @@ struct Workspace {
   size_t off_mx_x, off_mx_x_scales;                // x: codes [T_max][mx_code_row(H)], scales [T_max][mx_scale_row(H)]
   size_t off_mx_h, off_mx_h_scales;                // h: codes (mx_h_at), scales [N_max][mx_scale_row(I)]
   size_t off_mx_h_shared, off_mx_h_shared_scales;  // the shared expert's h
-  size_t bytes;           // what every call but the 4-bit FFN needs
-  size_t mx_bytes;        // what that one needs, and so all of them
+  // the 8-bit FFN's, over the same
+  size_t off_mx8_h, off_mx8_h_scales;                // h: codes [N_max][I], scales [N_max][I / 32]
+  size_t off_mx8_h_shared, off_mx8_h_shared_scales;  // the shared expert's h
+  size_t bytes;           // what every call but the 4-bit and the 8-bit FFN needs
+  size_t mx_bytes;        // what the 4-bit FFN needs
+  size_t mx8_bytes;       // what the 8-bit FFN needs
 };
 
 struct TimingSlot {
@@ -175,6 +179,9 @@ int launch_route_biased(revive_ctx*, const float* logits, const float* bias, boo
 int launch_mx_expert_ffn(revive_ctx*, const void* x, const int32_t* src_of, const int32_t* slot_offsets, const void* const* w_gate_up,
                          const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down, void* y_shared, int T,
                          hipStream_t);
+int launch_mx8_expert_ffn(revive_ctx*, const uint8_t* x, const uint8_t* x_scales, const int32_t* src_of, const int32_t* slot_offsets,
+                          const void* const* w_gate_up, const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down,
+                          void* y_shared, int T, hipStream_t);
 int launch_expert_counts(revive_ctx*, const int32_t* topk_logical, int T, int64_t* counts, hipStream_t);
 int launch_combine(revive_ctx*, const void* y_perm, const int32_t* dst_row, const float* topk_weight,
                    const void* y_shared, int T, void* out, hipStream_t);

@@ -1,0 +1,87 @@
+// Grouped SwiGLU expert FFN on microscaled 8-bit weights and activations.
+//
+// Paper: Sec. 2.1 (each expert acts as an FFN).  With Q the rounding of mx8.hpp, every slot p with rows
+// [slot_offsets[p], slot_offsets[p+1]) computes h = Q(silu(x G_p) * (x U_p)), y = h D_p, and the shared expert the same on all
+// tokens.  x comes in 8 bits (the norm in front of the layer gives it so); a routed row reads its token's codes through src_of,
+// so that dispatch need not copy rows.  Slots without rows produce no tile and their weights are never read.
+#include <algorithm>
+
+#include "ctx.hpp"
+#include "mx8_stream.hpp"
+
+namespace revive {
+
+namespace {
+
+struct Mx8Ffn {
+  const uint8_t* x; const uint8_t* x_scales;
+  const int32_t* src_of; const int32_t* slot_offsets; const void* const* w_gate_up; const void* const* w_down; void* y_perm;
+  const void* w_sh_gate_up; const void* w_sh_down; void* y_shared;
+  int N, T;  // routed rows, rows of the shared expert (0: none)
+};
+
+// One of the FFN's two products on the routed rows or on the shared expert's.
+template <int EPI>
+Mx8Problem mx8_problem(const revive_ctx* ctx, const Mx8Ffn& f, bool shared) {
+  const revive_config& c = ctx->cfg;
+  const Workspace& w = ctx->ws;
+  const int I = shared ? c.I_shared : c.I, rows = shared ? f.T : f.N;
+  uint8_t* h = ctx->d_ws + (shared ? w.off_mx8_h_shared : w.off_mx8_h);
+  uint8_t* h_scales = ctx->d_ws + (shared ? w.off_mx8_h_shared_scales : w.off_mx8_h_scales);
+  Mx8Problem p{};
+  p.n_out = EPI == EPI8_H ? I : c.H;
+  p.K = EPI == EPI8_H ? c.H : I;
+  p.b_codes = mx8_packed_codes(p.n_out, p.K);
+  p.a_row = p.K;
+  if (EPI == EPI8_H) {
+    p.A = f.x; p.A_scales = f.x_scales;
+    p.src_of = shared ? nullptr : f.src_of; p.k = c.k;
+    p.b_half = mx8_packed_bytes(I, c.H);
+    p.H = h; p.H_scales = h_scales;
+  } else {
+    p.A = h; p.A_scales = h_scales;
+    p.Y = static_cast<uint16_t*>(shared ? f.y_shared : f.y_perm);
+  }
+  if (shared) p.B_one = EPI == EPI8_H ? f.w_sh_gate_up : f.w_sh_down;
+  else p.B_tab = EPI == EPI8_H ? f.w_gate_up : f.w_down;
+  p.M = rows;
+  return p;
+}
+
+// A product's arguments for tiles of tile_m rows and `width` columns; false: more than one launch takes.
+template <int EPI>
+bool mx8_args(const revive_ctx* ctx, const Mx8Ffn& f, int tile_m, int width, int threads, Mx8Args& a) {
+  a = Mx8Args{};
+  a.slot_offsets = f.slot_offsets;
+  a.P = ctx->P;
+  a.grouped = mx8_problem<EPI>(ctx, f, false);
+  // as many row-tiles as the rows can make in the slots that can hold one
+  bool fits = mx8_cut(a.grouped, f.N / tile_m + std::min(f.N, ctx->P), width, threads);
+  if (f.T > 0) {
+    a.dense = mx8_problem<EPI>(ctx, f, true);
+    fits = mx8_cut(a.dense, ceil_div(f.T, tile_m), width, threads) && fits;
+  }
+  return fits;
+}
+
+int too_large(const revive_ctx* ctx) { return fail(ctx, REVIVE_EINVAL, "revive_mx_eight_expert_ffn: rows times columns are more than one launch takes"); }
+
+template <int TMX, int EPI>
+int mx8_stream_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
+  Mx8Args a;
+  if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 64, 256, a)) return too_large(ctx);
+  KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
+  return launch_mx8_stream<TMX, 4, 4, EPI>(ctx, a, stream);
+}
+
+}  // namespace
+
+int launch_mx8_expert_ffn(revive_ctx* ctx, const uint8_t* x, const uint8_t* x_scales, const int32_t* src_of, const int32_t* slot_offsets,
+                          const void* const* w_gate_up, const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down,
+                          void* y_shared, int T, hipStream_t stream) {
+  const Mx8Ffn f{x, x_scales, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * ctx->cfg.k, y_shared ? T : 0};
+  const int rc = mx8_stream_product<4, EPI8_H>(ctx, f, stream);
+  return rc != REVIVE_OK ? rc : mx8_stream_product<4, EPI8_Y>(ctx, f, stream);
+}
+
+}  // namespace revive

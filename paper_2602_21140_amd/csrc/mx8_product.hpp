@@ -1,0 +1,158 @@
+// The products of microscaled 8-bit activations and weights: what a launch is given, and what becomes of its sums.
+//
+//   C[rows of tile, n] = sum_k A[row, k] * B_group[n, k], fp32 sums
+//
+// Three epilogues: EPI8_H: B holds gate and up; store silu(gate) * up as microscaled 8-bit numbers (the next product's
+// activations).  EPI8_Y: store bf16.  EPI8_LINEAR: add a bias, apply an activation, add a residual, store bf16.
+#pragma once
+
+#include <type_traits>
+
+#include "ctx.hpp"
+#include "gemm_bf16.hpp"
+#include "mx8.hpp"
+#include "row_tiles.hpp"
+
+namespace revive {
+
+enum { EPI8_H = 0, EPI8_Y = 1, EPI8_LINEAR = 2 };
+
+struct Mx8Problem {
+  const uint8_t* A;          // codes of row r: A + r * a_row
+  int64_t a_row;
+  const uint8_t* A_scales;   // rows of ceil(K / 32) bytes
+  const int32_t* src_of;     // not null: row r of the product is row src_of[r] / k of A
+  int k;
+  const void* const* B_tab;  // device table slot -> packed weights (grouped), or
+  const void* B_one;         // the one packed matrix (dense)
+  int64_t b_half;            // EPI8_H: bytes from the gate matrix to the up matrix
+  int64_t b_codes;           // bytes from a matrix' codes to its scales
+  uint8_t* H; uint8_t* H_scales;  // EPI8_H: codes [rows, n_out], scales [rows, n_out / 32]
+  uint16_t* Y;               // bf16; EPI8_Y: [rows, n_out]; EPI8_LINEAR: rows ldy elements apart
+  int64_t ldy, ld_residual;
+  const float* bias; const uint16_t* residual;  // EPI8_LINEAR, may be null; the residual is bf16
+  int activation;
+  int n_out, K;
+  int n_col_tiles, n_row_tiles;
+  int blocks;                // workgroups of the grid that belong to this problem, a multiple of 8
+  int M;                     // rows (dense)
+};
+
+struct Mx8Args {
+  Mx8Problem dense;             // served by the first dense.blocks workgroups
+  Mx8Problem grouped;           // served by the others
+  const int32_t* slot_offsets;  // [P + 1]: rows of every slot (grouped)
+  int P;
+};
+
+// Cuts a problem into tiles of `width` columns and n_row_tiles row-tiles, for workgroups of `threads`.  A grid has fewer than 2^32
+// threads (a launch of more runs what is left of them modulo 2^32, without an error): false if it would have more, with what a
+// second problem of the same size adds.
+inline bool mx8_cut(Mx8Problem& p, int64_t n_row_tiles, int width, int threads) {
+  p.n_col_tiles = ceil_div(p.n_out, width);
+  const int64_t blocks = (n_row_tiles * p.n_col_tiles + 7) / 8 * 8;
+  if (blocks * threads >= (1ll << 31)) return false;
+  p.n_row_tiles = static_cast<int>(n_row_tiles);
+  p.blocks = static_cast<int>(blocks);
+  return true;
+}
+
+typedef int32_t mx8_i32x8 __attribute__((ext_vector_type(8)));
+typedef float mx8_f32x4 __attribute__((ext_vector_type(4)));
+struct Mx8Frag { mx8_u32x4 half[2]; };  // a lane's codes of 128 K-elements of a row
+
+// The matrix cores add up fp8 products in groups of 8 consecutive K-elements: a group's products are brought to a unit of 2^-13 of
+// the power of two of its largest and cut off there (measured, with powers of two beside each other), and the groups' sums and the
+// accumulator are added to 24 bits.  A product's result is off by 3e-5 of its size so (normally distributed operands): enough for
+// results in 16 or 8 bits, and why there are none in 32.
+//
+// acc[4 (l / 16) + i of the first operand's rows][l % 16 of the second's] += 128 products; byte S of each scale word.
+template <int SW, int SX>
+__device__ __forceinline__ mx8_f32x4 mx8_mfma(const Mx8Frag& w, const Mx8Frag& x, mx8_f32x4 acc, uint32_t w_scale, uint32_t x_scale) {
+  mx8_i32x8 a, b;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    a[i] = static_cast<int>(w.half[i >> 2][i & 3]);
+    b[i] = static_cast<int>(x.half[i >> 2][i & 3]);
+  }
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, SW, static_cast<int>(w_scale), SX, static_cast<int>(x_scale));
+}
+
+template <typename F, int... S>
+__device__ __forceinline__ void mx8_for(std::integer_sequence<int, S...>, F f) { (f(std::integral_constant<int, S>{}), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void mx8_for_blocks(F f) { mx8_for(std::make_integer_sequence<int, N>{}, f); }
+
+// Rows and weights of workgroup `blockIdx.x`; row_begin >= row_end: nothing to do.
+struct Mx8Tile { const uint8_t* B; int n_idx, row_begin, row_end; bool once; };  // once: nobody else reads these weights
+__device__ __forceinline__ Mx8Tile mx8_tile_of(const Mx8Args& a, const Mx8Problem& g, bool dense, int tile_m) {
+  Mx8Tile t{nullptr, 0, 0, 0, true};
+  if (dense) {
+    // each XCD (workgroup i runs on XCD i % 8) takes a contiguous eighth of the tiles, row-tiles of the same weights together
+    const int at = (blockIdx.x & 7) * (g.blocks >> 3) + (blockIdx.x >> 3);
+    if (at >= g.n_col_tiles * g.n_row_tiles) return t;
+    t.n_idx = at / g.n_row_tiles;
+    t.row_begin = (at - t.n_idx * g.n_row_tiles) * tile_m;
+    t.row_end = min(g.M, t.row_begin + tile_m);
+    t.B = static_cast<const uint8_t*>(g.B_one);
+    t.once = g.n_row_tiles == 1;
+  } else {
+    const GridTile r = grid_tile(a.slot_offsets, a.P, tile_m, g.n_col_tiles, blockIdx.x - a.dense.blocks, g.B_tab);
+    if (r.group < 0) return t;
+    t.B = static_cast<const uint8_t*>(r.w);
+    t.n_idx = r.n_idx;
+    t.row_begin = r.row_begin;
+    t.row_end = r.row_end;
+    t.once = r.in_group == 1;
+  }
+  return t;
+}
+
+// The lane's eight columns of gate and up of one row, of a block of 32 columns that the lanes l, l ^ 16, l ^ 32, l ^ 48 share
+// -> two words of codes, and the block's scale byte.
+__device__ __forceinline__ uint2 mx8_swiglu_codes(const mx8_f32x4& g0, const mx8_f32x4& g1, const mx8_f32x4& u0, const mx8_f32x4& u1, uint32_t& byte) {
+  float v[8];
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = i < 4 ? silu_f32(g0[i & 3]) * u0[i & 3] : silu_f32(g1[i & 3]) * u1[i & 3];
+    m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  }
+  m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+  m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
+  byte = mx8_scale_byte(m);
+  return mx8_codes8(v, byte);
+}
+
+// Functions of the linear product's epilogue, as exact as the functions they call.
+__device__ __forceinline__ float mx8_activated(float z, int activation) {
+  switch (activation) {
+    case REVIVE_ACT_RELU: return z < 0.f ? 0.f : z;  // a NaN stays one
+    case REVIVE_ACT_SILU: return silu_f32(z);
+    case REVIVE_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752f * z);  // z times the normal distribution's function
+    default: return z;
+  }
+}
+
+// Eight consecutive columns from `col` on (a multiple of 8) of one row.
+__device__ __forceinline__ void mx8_store_linear(const Mx8Problem& g, int row, int col, float* v) {
+  if (col >= g.n_out) return;
+  uint32_t bits[8];
+  if (g.bias) {
+    mx8_load8<float, false>(g.bias, col, g.n_out, bits);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(bits[i]);
+  }
+  if (g.activation != REVIVE_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = mx8_activated(v[i], g.activation);
+  }
+  if (g.residual) {
+    mx8_load8<uint16_t, false>(g.residual + row * g.ld_residual, col, g.n_out, bits);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(bits[i]);
+  }
+  mx8_store8<uint16_t, false>(g.Y + row * g.ldy, col, g.n_out, v);
+}
+
+}  // namespace revive

@@ -1,0 +1,188 @@
+// Product of microscaled 8-bit activations and weights for few rows: the weights are streamed once, straight into registers.
+//
+// A workgroup covers up to 16 TMX rows and W 16-row blocks of weight rows (EPI8_H: half of them gate, half up).  Its NW
+// wavefronts share K, each with a contiguous part of the steps of 128, and add up their sums through LDS at the end, in the
+// wavefronts' order.  So the K loop has no barrier and no LDS, and a product of few columns still has many wavefronts: what
+// bounds it is how fast HBM is read, and in the smallest calls latency.  Weights and activations of the next two steps are on
+// their way in registers.
+#pragma once
+
+#include "mx8_product.hpp"
+
+namespace revive {
+
+template <int TMX, int W, int NW, int EPI>
+constexpr size_t mx8_stream_lds() { return static_cast<size_t>(NW) * W * TMX * 1024; }
+
+template <int TMX, int W, int NW, int EPI>
+__global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
+  static_assert(W % 2 == 0 && W <= 4 && (EPI != EPI8_H || W == 4) && NW > 1, "output columns in sets of 32, sums by way of LDS");
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const bool dense = blockIdx.x < static_cast<unsigned>(a.dense.blocks);
+  const Mx8Problem g = dense ? a.dense : a.grouped;
+  const Mx8Tile t = mx8_tile_of(a, g, dense, 16 * TMX);
+  if (t.row_begin >= t.row_end) return;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, kb = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = t.row_end - t.row_begin;
+  const int KT = mx8_steps(g.K), blocks = g.K / kMx8Block;
+
+  // 16-row blocks of weights: where a lane's codes and scales of step 0 are
+  constexpr int PER = W < 4 ? W : W / (EPI == EPI8_H ? 2 : 1);  // blocks side by side in a panel
+  const int block0 = t.n_idx * PER, panel = block0 >> 3, sub0 = block0 & 7;
+  const uint8_t* codes[W];
+  const uint8_t* scales[EPI == EPI8_H ? 2 : 1];
+#pragma unroll
+  for (int s = 0; s < W; ++s)
+    codes[s] = t.B + (EPI == EPI8_H && s >= W / 2 ? g.b_half : 0) + static_cast<int64_t>(panel) * KT * kMx8PanelStep + (sub0 + s % PER) * 2048 + lane * 16;
+#pragma unroll
+  for (int h = 0; h < (EPI == EPI8_H ? 2 : 1); ++h)
+    scales[h] = t.B + (h ? g.b_half : 0) + g.b_codes + static_cast<int64_t>(panel) * KT * kMx8PanelScales + lane * 8 + sub0;
+  auto source = [&](int r) -> int64_t {  // row of A; rows past the tile read its last row again
+    const int row = t.row_begin + min(r, rows - 1);
+    return g.src_of ? g.src_of[row] / g.k : row;
+  };
+
+  auto run = [&](auto tm_tag, auto once_tag) {
+    constexpr int TM = decltype(tm_tag)::value;
+    constexpr bool ONCE = decltype(once_tag)::value;  // streamed past the caches' retention (non-temporal)
+    const uint8_t* x[TM];
+    const uint8_t* xs[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t row = source(i * 16 + r16);
+      x[i] = g.A + row * g.a_row + kb * 16;
+      xs[i] = g.A_scales + row * blocks;
+    }
+    mx8_f32x4 acc[W][TM];
+#pragma unroll
+    for (int s = 0; s < W; ++s)
+#pragma unroll
+      for (int i = 0; i < TM; ++i) acc[s][i] = mx8_f32x4{0.f, 0.f, 0.f, 0.f};
+
+    struct Step { Mx8Frag w[W], x[TM]; uint32_t ws, xs[TM]; };
+    auto word = [](const uint8_t* p) { typedef uint32_t any __attribute__((aligned(1))); return *reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(p)); };
+    auto load_w = [&](Step& b, int step) {
+#pragma unroll
+      for (int s = 0; s < W; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(codes[s] + static_cast<int64_t>(step) * kMx8PanelStep + h * 1024));
+          b.w[s].half[h] = ONCE ? __builtin_nontemporal_load(p) : *p;
+        }
+      const int64_t at = static_cast<int64_t>(step) * kMx8PanelScales;
+      auto two = [&](const uint8_t* p) { return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) uint16_t*>(reinterpret_cast<uintptr_t>(p + at))); };
+      if (EPI == EPI8_H) b.ws = two(scales[0]) | two(scales[1]) << 16;
+      else if (W == 2) b.ws = two(scales[0]);
+      else b.ws = word(scales[0] + at);
+    };
+    auto multiply = [&](const Step& b) {
+      mx8_for_blocks<W>([&](auto s) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[s.value][i] = mx8_mfma<s.value, 0>(b.w[s.value], b.x[i], acc[s.value][i], b.ws, b.xs[i]);
+      });
+    };
+    auto load = [&](Step& b, int step) {  // a whole step
+      load_w(b, step);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b.x[i].half[h] = *reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i] + static_cast<int64_t>(step) * kMx8Step + h * 64));
+        b.xs[i] = word(xs[i] + step * 4);  // the step's four blocks; a lane's own goes to byte 0 before use
+      }
+    };
+    auto own_scales = [&](Step& b) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) b.xs[i] >>= kb * 8;
+    };
+
+    const int whole = g.K / kMx8Step;
+    const int first = wave * whole / NW, last = (wave + 1) * whole / NW;  // KT < 2^18
+    if (first < last) {
+      Step b[2];
+      load(b[0], first);
+      load(b[1], min(first + 1, last - 1));
+      int s = first;
+      for (; s + 2 <= last; s += 2) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          own_scales(b[u]);
+          multiply(b[u]);
+          load(b[u], min(s + u + 2, last - 1));  // past the last step that one again, not multiplied
+        }
+      }
+      if (s < last) {
+        own_scales(b[0]);
+        multiply(b[0]);
+      }
+    }
+    if (wave == NW - 1 && whole < KT) {  // what is left of K, a multiple of 32: zeros behind it, and scales of 2^-127
+      Step b;
+      load_w(b, whole);
+      const int left = g.K - whole * kMx8Step;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bool in = h * 64 + kb * 16 < left;
+          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i] + (in ? static_cast<int64_t>(whole) * kMx8Step + h * 64 : -kb * 16));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) b.x[i].half[h][j] = in ? v[j] : 0u;
+        }
+        b.xs[i] = kb * 32 < left ? xs[i][whole * 4 + kb] : 0u;
+      }
+      multiply(b);
+    }
+
+    // the wavefronts' sums, tile by tile; NW tiles at a time are added up, a wavefront each its own
+    mx8_f32x4* part = reinterpret_cast<mx8_f32x4*>(smem);
+    if (NW > 1) {
+#pragma unroll
+      for (int s = 0; s < W; ++s)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) part[((wave * W + s) * TM + i) * 64 + lane] = acc[s][i];
+      __syncthreads();
+    }
+    auto total = [&](int s, int i) {
+      mx8_f32x4 v = part[(s * TM + i) * 64 + lane];
+      for (int w = 1; w < NW; ++w) v += part[((w * W + s) * TM + i) * 64 + lane];
+      return v;
+    };
+    // a lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16
+    constexpr int PAIRS = EPI == EPI8_H ? 1 : W / 2;
+    for (int item = wave; item < TM * PAIRS; item += NW) {
+      const int i = item / PAIRS, p = item - i * PAIRS;
+      const int row = t.row_begin + i * 16 + r16, col = (block0 + 2 * p) * 16 + kb * 8;
+      const mx8_f32x4 v0 = total(2 * p, i), v1 = total(2 * p + 1, i);
+      if (EPI == EPI8_H) {
+        uint32_t byte;
+        const uint2 out = mx8_swiglu_codes(v0, v1, total(2, i), total(3, i), byte);
+        if (row >= t.row_end || col >= g.n_out) continue;
+        *reinterpret_cast<uint2*>(g.H + static_cast<int64_t>(row) * g.n_out + col) = out;
+        if (kb == 0) g.H_scales[static_cast<int64_t>(row) * (g.n_out >> 5) + (col >> 5)] = static_cast<uint8_t>(byte);
+      } else if (row < t.row_end) {
+        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        if (EPI == EPI8_LINEAR) mx8_store_linear(g, row, col, v);
+        else if (col < g.n_out) mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(row) * g.n_out, col, g.n_out, v);
+      }
+    }
+  };
+  using Y = std::true_type;
+  if (!t.once) run(std::integral_constant<int, TMX>{}, std::false_type{});
+  else if (TMX == 1 || rows <= 16) run(std::integral_constant<int, 1>{}, Y{});
+  else if (TMX == 2 || rows <= 32) run(std::integral_constant<int, (TMX < 2 ? TMX : 2)>{}, Y{});
+  else run(std::integral_constant<int, TMX>{}, Y{});
+}
+
+template <int TMX, int W, int NW, int EPI>
+int launch_mx8_stream(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
+  const int grid = args.dense.blocks + args.grouped.blocks;
+  if (grid <= 0) return REVIVE_OK;
+  constexpr size_t lds = mx8_stream_lds<TMX, W, NW, EPI>();
+  auto kern = mx8_stream_kernel<TMX, W, NW, EPI>;
+  if (lds > 64 * 1024) REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * NW), lds, stream, args);
+  return check_hip(ctx, hipGetLastError(), "mx8_stream launch");
+}
+
+}  // namespace revive

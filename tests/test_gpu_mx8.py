@@ -1,0 +1,322 @@
+"""Microscaled 8-bit floats and the expert FFN on them against the oracle in 64 bits."""
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+import torch
+
+from harness import f64
+from oracle import mx8_oracle as mx
+from oracle import revive_oracle as orc
+from paper_2602_21140_amd import ReviveError, ReviveLayer, binding, mx8_dequantize, mx8_pack, mx8_pack_expert, mx8_quantize
+from test_gpu_mx import make_rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,K", [(1, 1), (1, 32), (3, 31), (5, 33), (64, 64), (7, 129), (130, 1000), (33, 4104), (2, 16384), (1025, 96)])
+def test_quantize_and_back(rows, K, dtype):
+    x = make_rows(rows, K, dtype, rows + K)
+    codes, scales = mx8_quantize(x)
+    want_codes, want_scales = mx.quantize(f64(x))
+    assert np.array_equal(scales.cpu().numpy(), want_scales)
+    assert np.array_equal(codes.cpu().numpy(), want_codes)
+    want = mx.values(want_codes, want_scales)[:, :K]
+    assert np.array_equal(f64(mx8_dequantize(codes, scales, K, dtype=torch.float32)), want)
+    as_bf16 = torch.from_numpy(want).float().to(torch.bfloat16)  # exact, but for numbers below 2^-133
+    assert torch.equal(mx8_dequantize(codes, scales, K).cpu(), as_bf16)
+
+
+def test_every_code_and_scale_back():
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1).cuda()
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 8).cuda()
+    want = mx.values(codes.cpu().numpy(), scales.cpu().numpy())
+    with np.errstate(over="ignore"):
+        want = want.astype(np.float32).astype(np.float64)  # 448 * 2^127 is beyond fp32
+    got = f64(mx8_dequantize(codes, scales, dtype=torch.float32))
+    assert np.array_equal(got, want, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_strided_and_unaligned_rows(dtype):
+    base = make_rows(40, 300, dtype, 3)
+    for x in (base[:, 5:261], base[::2, 8:264], base[1:, 1:2], base[:, :256]):
+        codes, scales = mx8_quantize(x)
+        want_codes, want_scales = mx.quantize(f64(x))
+        assert np.array_equal(codes.cpu().numpy(), want_codes) and np.array_equal(scales.cpu().numpy(), want_scales)
+        out = torch.full((40, 300), 7.0, dtype=dtype, device="cuda")
+        part = out[:len(x), 3:3 + x.shape[1]]
+        mx8_dequantize(codes, scales, out=part)
+        want = torch.from_numpy(mx.values(want_codes, want_scales)[:, :x.shape[1]]).float().to(dtype)
+        assert torch.equal(part.cpu(), want)
+        part.fill_(7.0)
+        assert bool((out == 7.0).all())  # nothing beside the rows was written
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_not_finite_blocks_are_nan_and_alone(dtype):
+    x = make_rows(4, 160, dtype, 9)
+    x[0, 40], x[1, 0], x[2, 159], x[3, 70] = float("nan"), float("inf"), -float("inf"), 3e38
+    codes, scales = mx8_quantize(x)
+    want_codes, want_scales = mx.quantize(f64(x))
+    assert np.array_equal(scales.cpu().numpy(), want_scales) and np.array_equal(codes.cpu().numpy(), want_codes)
+    v = f64(mx8_dequantize(codes, scales))
+    assert np.isnan(v).sum() == 3 * 32 and np.isnan(v[0, 32:64]).all() and np.isnan(v[1, :32]).all() and np.isnan(v[2, 128:]).all()
+
+
+def test_quantize_of_no_rows_and_on_another_stream():
+    codes, scales = mx8_quantize(torch.empty(0, 64, device="cuda"))
+    assert codes.shape == (0, 64) and scales.shape == (0, 2) and mx8_dequantize(codes, scales).shape == (0, 64)
+    s = torch.cuda.Stream()
+    x = make_rows(64, 512, torch.float32, 1)
+    s.wait_stream(torch.cuda.current_stream())
+    codes, scales = mx8_quantize(x, stream=s)
+    s.synchronize()
+    assert np.array_equal(codes.cpu().numpy(), mx.quantize(f64(x))[0])
+
+
+@pytest.mark.parametrize("rows,K", [(64, 32), (128, 128), (130, 704), (320, 576), (1, 96)])
+def test_packed_layout(rows, K):
+    """Every byte of the layout that the header states."""
+    codes, scales = mx.quantize(np.random.default_rng(K).standard_normal((rows, K)))
+    packed = mx8_pack(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()).cpu().numpy()
+    panels, steps = -(-rows // 128), -(-K // 128)
+    assert packed.size == binding.mx8_packed_bytes(rows, K) == panels * 128 * steps * 132
+    c = packed[:panels * 128 * steps * 128].reshape(panels, steps, 8, 2, 64, 16)
+    s = packed[c.size:].reshape(panels, steps, 64, 8)
+    full = np.zeros((panels * 128, steps * 128), np.uint8)
+    full[:rows, :K] = codes
+    full_s = np.zeros((panels * 128, steps * 4), np.uint8)
+    full_s[:rows, :K // 32] = scales
+    for sub in range(8):
+        for lane in range(64):
+            m = lane % 16
+            r = np.arange(panels) * 128 + 32 * (sub // 2) + 8 * (m // 4) + 4 * (sub % 2) + m % 4
+            for st in range(steps):
+                for h in range(2):
+                    at = st * 128 + 64 * h + 16 * (lane // 16)
+                    assert np.array_equal(c[:, st, sub, h, lane], full[r, at:at + 16])
+                assert np.array_equal(s[:, st, lane, sub], full_s[r, st * 4 + lane // 16])
+
+
+# ---- the expert FFN ------------------------------------------------------------------------------
+
+
+def sum_error(a, m):
+    """The matrix cores cut each of 8 consecutive products off at 2^-13 of the largest one's power of two; these groups' sums, the
+    accumulator and the sums of wavefronts that share K are added in fp32, cut off at 2^-23 of what is there."""
+    def groups(v):  # largest magnitude of 8 along the last axis
+        return np.abs(np.pad(v, ((0, 0), (0, -v.shape[1] % 8)))).reshape(len(v), -1, 8).max(axis=2)
+    return 8 * 2.0 ** -13 * (groups(a) @ groups(m.T).T) + (a.shape[1] / 8 + 16) * 2.0 ** -23 * (np.abs(a) @ np.abs(m))
+
+
+def check_ffn(y, x, w, what):
+    """Element by element.  h is off by what its two sums and a few roundings in silu make; where its rounding to 8 bits (or its
+    block's scale) hangs on less than that, either result is right, and y may differ by the step times the weight.  Then y's own
+    sum and its rounding to bf16 (2^-8)."""
+    g, u = x @ w["gate"], x @ w["up"]
+    h = orc.silu(g) * u
+    # |silu'| <= 1.1, |silu(g)| <= |g|
+    dh = 1.1 * sum_error(x, w["gate"]) * (np.abs(u) + sum_error(x, w["up"])) + np.abs(orc.silu(g)) * sum_error(x, w["up"]) + 2.0 ** -20 * np.abs(h)
+    ref = mx.rounded(h)
+    largest, slack = np.abs(h), np.zeros_like(h)
+    for scales in (mx.scale_bytes(np.maximum(largest - dh, 0)), mx.scale_bytes(largest + dh)):
+        step = np.exp2(scales.astype(np.float64) - 127).repeat(32, axis=1)[:, :h.shape[1]]
+        for moved in (h - dh, h + dh):
+            v = mx.grid_values(mx.codes_for(moved, scales).reshape(len(h), -1)[:, :h.shape[1]]) * step
+            slack = np.maximum(slack, np.abs(v - ref))
+    want = ref @ w["down"]
+    allowed = slack @ np.abs(w["down"]) + sum_error(np.abs(ref) + slack, w["down"]) + 2.0 ** -8 * np.abs(want) + 1e-30
+    off = np.abs(y - want)
+    assert np.isfinite(y).all(), what
+    assert (off <= allowed).all(), (what, float((off / allowed).max()), np.argwhere(off > allowed)[:4].tolist())
+    # All elements together, whose errors are independent: bf16's rounding is evenly spread, 2^-8 / sqrt(3) of them; of h, an error d
+    # moves a number to the next code, s away, with the probability d / s, in the mean square d s: with d below 2^-12 of h's size and
+    # s 2^-3 of it, 2^-7.5 of y.
+    if y.size >= 1000:
+        assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want), what
+
+
+class Ffn:
+    """A layer of random 8-bit experts with a given number of rows per slot, and its oracle."""
+
+    def __init__(self, H, I, k, rows_per_slot, I_shared=0, T=None, seed=0):
+        rng = np.random.default_rng(seed)
+        self.H, self.I, self.P, self.k = H, I, len(rows_per_slot), k
+        n = int(sum(rows_per_slot))
+        self.T = T = -(-n // k) if T is None else T
+        self.N = T * k
+        assert n <= self.N
+        cfg = SimpleNamespace(T=T, H=H, E=max(self.P, k), k=k, I=I, I_shared=I_shared, n_ranks=1, slots_per_rank=self.P, max_replicas=1,
+                              score_fn="softmax", n_group=1, topk_group=1, dtype="bf16")
+        self.L = ReviveLayer(cfg)
+        self.L.workspace.fill_(255)  # what a kernel reads before it is written shows as NaN
+        self.L._check(self.L.L.revive_bind_workspace(self.L._ctx, self.L.workspace.data_ptr(), self.L.workspace.numel()))
+        self.x = torch.from_numpy(rng.standard_normal((T, H))).to(torch.bfloat16).cuda()
+        self.form = mx8_quantize(self.x)
+        self.offsets = np.concatenate([[0], np.cumsum(rows_per_slot)]).astype(np.int32)
+        self.src_of = rng.permutation(self.N).astype(np.int32)
+        self.experts, gu, dn = [], [], []
+        for p in range(self.P):
+            if not rows_per_slot[p]:  # a slot without rows: there is nothing to point at
+                gu.append(None), dn.append(None), self.experts.append(None)
+                continue
+            w = self._draw(rng, I)
+            self.experts.append(mx.expert_values({n: f64(t) for n, t in w.items()}))
+            a, b = mx8_pack_expert(w["gate"], w["up"], w["down"])
+            gu.append(a), dn.append(b)
+        self.L.set_mx8_expert_weights(gu, dn)
+        self.shared, self.sh = None, (None, None)
+        if I_shared:
+            w = self._draw(rng, I_shared)
+            self.shared, self.sh = mx.expert_values({n: f64(t) for n, t in w.items()}), mx8_pack_expert(w["gate"], w["up"], w["down"])
+        self.d_offsets, self.d_src = torch.from_numpy(self.offsets).cuda(), torch.from_numpy(self.src_of).cuda()
+
+    def _draw(self, rng, I):
+        shape = {"gate": (self.H, I), "up": (self.H, I), "down": (I, self.H)}
+        return {n: torch.from_numpy(rng.standard_normal(s) * self.H ** -0.5).float().cuda() for n, s in shape.items()}
+
+    def run(self, **kw):
+        out = (torch.full((self.N, self.H), 5.0, dtype=torch.bfloat16, device="cuda"),
+               torch.full((self.T, self.H), 5.0, dtype=torch.bfloat16, device="cuda") if self.shared else None)
+        return self.L.mx8_expert_ffn(*self.form, self.d_src, self.d_offsets, self.T, *self.sh, out=out, **kw)
+
+    def check(self, y, y_shared):
+        y, x, n = f64(y), mx.rounded(f64(self.x)), int(self.offsets[-1])
+        for p, w in enumerate(self.experts):
+            a, b = self.offsets[p], self.offsets[p + 1]
+            if a < b:
+                check_ffn(y[a:b], x[self.src_of[a:b] // self.k], w, ("slot", p))
+        assert (y[n:] == 5.0).all()  # rows of no slot are left alone
+        if self.shared:
+            check_ffn(f64(y_shared), x, self.shared, "shared")
+
+
+# hidden and intermediate sizes that end inside a step (128) and a panel of rows (128), K below a step and with fewer steps than
+# wavefronts share; slots with one row, none, a full tile, one more; rows that fill several tiles
+SHAPES = [(64, 64, 1, [1]), (64, 64, 2, [0, 2, 0]), (192, 320, 1, [5, 0, 17]), (128, 128, 4, [16, 1, 0, 3]), (576, 704, 2, [33, 7, 64]),
+          (1088, 192, 3, [65, 0, 1, 129]), (640, 1088, 1, [300, 2]), (2112, 512, 6, [40] * 6), (1024, 256, 1, [512]), (960, 448, 2, [257, 255, 256])]
+
+
+@pytest.mark.parametrize("H,I,k,rows", SHAPES)
+def test_ffn(H, I, k, rows):
+    f = Ffn(H, I, k, rows, seed=H + I)
+    f.check(*f.run())
+    f.L.close()
+
+
+@pytest.mark.parametrize("H,I,I_shared,k,rows,T", [(128, 64, 64, 1, [1], 1), (192, 128, 320, 2, [3, 0, 5], 37), (576, 320, 192, 2, [100, 0, 30], 131),
+                                                   (320, 64, 1088, 1, [0, 0], 300), (1088, 704, 576, 2, [700, 0, 500], 600)])
+def test_ffn_with_shared_expert(H, I, I_shared, k, rows, T):
+    f = Ffn(H, I, k, rows, I_shared, T, seed=T)
+    f.check(*f.run())
+    f.L.close()
+
+
+@pytest.mark.parametrize("rows,T", [([9, 20, 0, 40], 35), ([300, 0, 200, 100], 300)])
+def test_ffn_rows_that_are_not_finite_stay_alone(rows, T):
+    f = Ffn(192, 128, 2, rows, 64, T, seed=4)
+    n = sum(rows)
+    clean, clean_shared = (t.clone() for t in f.run())
+    bad = {3: float("nan"), 20: float("inf")}
+    for t, v in bad.items():
+        f.x[t, 77] = v
+    f.form = mx8_quantize(f.x)
+    y, shared = f.run()
+    touched = np.isin(f.src_of[:n] // 2, list(bad))
+    y, clean = f64(y)[:n], f64(clean)[:n]
+    assert np.isnan(y[touched]).all() and np.array_equal(y[~touched], clean[~touched])
+    others = [t for t in range(f.T) if t not in bad]
+    assert np.isnan(f64(shared)[list(bad)]).all() and np.array_equal(f64(shared)[others], f64(clean_shared)[others])
+    f.L.close()
+
+
+@pytest.mark.parametrize("rows,T", [([100, 0, 30, 1], 80), ([600, 1, 0, 300], 500)])
+def test_ffn_is_deterministic_on_any_stream_and_in_a_graph(rows, T):
+    f = Ffn(576, 320, 2, rows, 192, T=T, seed=11)
+    y, shared = f.run()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = (torch.zeros_like(y), torch.zeros_like(shared))
+    f.L.mx8_expert_ffn(*f.form, f.d_src, f.d_offsets, f.T, *f.sh, out=out, stream=s)
+    s.synchronize()
+    n = f.offsets[-1]
+    assert torch.equal(out[0][:n], y[:n]) and torch.equal(out[1], shared)
+    f.L.graph_begin(s)
+    f.L.mx8_expert_ffn(*f.form, f.d_src, f.d_offsets, f.T, *f.sh, out=out, stream=s)
+    graph = f.L.graph_end(s)
+    x = f.x.clone()
+    for i in range(4):  # other inputs between the replays, and eager work
+        mx8_quantize(x * (i - 1.5), out=f.form)
+        want = f.run()
+        out[0].zero_(), out[1].zero_()
+        torch.cuda.synchronize()
+        f.L.graph_launch(graph, s)
+        s.synchronize()
+        assert torch.equal(out[0][:n], want[0][:n]) and torch.equal(out[1], want[1])
+    f.L.close()
+
+
+# ---- refusals ------------------------------------------------------------------------------------
+
+
+def test_quantize_refuses():
+    x = torch.zeros(4, 64, device="cuda")
+    with pytest.raises(TypeError):
+        mx8_quantize(x.half())
+    with pytest.raises(ValueError):
+        mx8_quantize(x.t())
+    with pytest.raises(ValueError):
+        mx8_quantize(x[0])
+    codes, scales = mx8_quantize(x)
+    with pytest.raises(ValueError):
+        mx8_quantize(x, out=(codes, scales[:2]))
+    with pytest.raises(ValueError):
+        mx8_dequantize(codes, scales, 33 * 3)
+    with pytest.raises(ValueError):
+        mx8_dequantize(codes[:, 1:], scales)
+    with pytest.raises(TypeError):
+        mx8_dequantize(codes, scales, dtype=torch.float16)
+    L = binding.lib()
+    p = codes.data_ptr()
+    for args in ((0, 1, 4, 64, 64, p, p, None), (p, 2, 4, 64, 64, p, p, None), (p, 1, -1, 64, 64, p, p, None), (p, 1, 4, 0, 64, p, p, None),
+                 (p, 1, 4, 64, 63, p, p, None), (p, 1, 4, 64, 64, p + 8, p, None), (p + 1, 1, 4, 64, 64, p, p, None), (p, 1, 4, 64, 64, p, 0, None)):
+        assert L.revive_mx_eight_quantize(*args) == -1 and L.revive_last_error(None)
+    for args in ((0, p, 4, 64, 1, p, 64, None), (p, p, 4, 64, 3, p, 64, None), (p, p, 4, 64, 1, p + 1, 64, None), (p, p, 4, 64, 1, p, 60, None)):
+        assert L.revive_mx_eight_dequantize(*args) == -1
+    with pytest.raises(ReviveError):
+        binding.mx8_packed_bytes(4, 33)
+    assert L.revive_mx_eight_pack(p, p, 4, 64, p + 4, None) == -1 and L.revive_mx_eight_pack(0, p, 4, 64, p, None) == -1
+    torch.cuda.synchronize()
+
+
+def test_ffn_refuses():
+    f = Ffn(64, 64, 1, [3], seed=1)
+    L, tabs = f.L, f.L._mx8_tabs
+    y = torch.empty(f.N, 64, dtype=torch.bfloat16, device="cuda")
+    good = [f.form[0].data_ptr(), f.form[1].data_ptr(), f.d_src.data_ptr(), f.d_offsets.data_ptr(), tabs[0].data_ptr(), tabs[1].data_ptr(), y.data_ptr(),
+            None, None, None, f.T, None]
+
+    def status(**change):
+        a = list(good)
+        for i, v in change.items():
+            a[int(i[1:])] = v
+        return L.L.revive_mx_eight_expert_ffn(L._ctx, *a)
+
+    for i in range(7):
+        assert status(**{f"_{i}": None}) == -1
+    assert status(_10=-1) == -1 and status(_10=f.T + 1) == -1
+    assert status(_9=y.data_ptr()) == -1                       # the layer has no shared expert
+    assert status(_6=y.data_ptr() + 8) == -1 and status(_0=f.form[0].data_ptr() + 8) == -1
+    assert status(_10=0) == 0
+    with pytest.raises(AssertionError):
+        L.set_mx8_expert_weights([torch.zeros(3, dtype=torch.uint8, device="cuda")], [None])
+    small = torch.empty(L.workspace.numel() // 2 // 256 * 256, dtype=torch.uint8, device="cuda")
+    assert L.L.revive_bind_workspace(L._ctx, small.data_ptr(), small.numel()) != 0  # and the bound one stays
+    L.close()
+    cfg = SimpleNamespace(T=2, H=64, E=1, k=1, I=64, I_shared=0, n_ranks=1, slots_per_rank=1, max_replicas=1, score_fn="softmax", n_group=1,
+                          topk_group=1, dtype="fp32")
+    fp32 = ReviveLayer(cfg)
+    assert fp32.L.revive_mx_eight_expert_ffn(fp32._ctx, *good) == -1
+    fp32.close()
