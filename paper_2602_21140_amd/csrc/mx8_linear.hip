@@ -2,6 +2,7 @@
 //   out = act(x W^T + bias) + residual
 #include "ctx.hpp"
 #include "mx8_stream.hpp"
+#include "mx8_tile.hpp"
 
 namespace revive {
 
@@ -15,6 +16,14 @@ int linear_stream(const Mx8Problem& base, hipStream_t stream) {
   a.dense = base;
   if (!mx8_cut(a.dense, ceil_div(base.M, 16 * TMX), 16 * W, 64 * NW)) return too_large();
   return launch_mx8_stream<TMX, W, NW, EPI8_LINEAR>(nullptr, a, stream);
+}
+
+template <int TM, int TN>
+int linear_tile(const Mx8Problem& base, hipStream_t stream) {
+  Mx8Args a{};
+  a.dense = base;
+  if (!mx8_cut(a.dense, ceil_div(base.M, 32 * TM), 64 * TN, 512)) return too_large();
+  return launch_mx8_tile<TM, TN, EPI8_LINEAR>(nullptr, a, stream);
 }
 
 }  // namespace
@@ -48,5 +57,7 @@ extern "C" int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales,
   p.n_out = N; p.K = K; p.M = rows;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (rows <= 16) return linear_stream<1, 2, 8>(p, s);
-  return linear_stream<4, 4, 4>(p, s);
+  if (rows <= 128 || K < 64) return linear_stream<4, 4, 4>(p, s);  // the tiles take K from two blocks on
+  if (static_cast<int64_t>(rows) * N < 256 * 256 * 256) return linear_tile<4, 2>(p, s);
+  return linear_tile<8, 4>(p, s);
 }

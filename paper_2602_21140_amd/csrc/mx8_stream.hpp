@@ -64,12 +64,10 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
     auto word = [](const uint8_t* p) { typedef uint32_t any __attribute__((aligned(1))); return *reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(p)); };
     auto load_w = [&](Step& b, int step) {
 #pragma unroll
-      for (int s = 0; s < W; ++s)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(codes[s] + static_cast<int64_t>(step) * kMx8PanelStep + h * 1024));
-          b.w[s].half[h] = ONCE ? __builtin_nontemporal_load(p) : *p;
-        }
+      for (int s = 0; s < W; ++s) {
+        const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(codes[s] + static_cast<int64_t>(step) * kMx8PanelStep));
+        b.w[s] = ONCE ? mx8_frag(__builtin_nontemporal_load(p), __builtin_nontemporal_load(p + 64)) : mx8_frag(p[0], p[64]);
+      }
       const int64_t at = static_cast<int64_t>(step) * kMx8PanelScales;
       auto two = [&](const uint8_t* p) { return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) uint16_t*>(reinterpret_cast<uintptr_t>(p + at))); };
       if (EPI == EPI8_H) b.ws = two(scales[0]) | two(scales[1]) << 16;
@@ -86,8 +84,8 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
       load_w(b, step);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) b.x[i].half[h] = *reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i] + static_cast<int64_t>(step) * kMx8Step + h * 64));
+        const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i] + static_cast<int64_t>(step) * kMx8Step));
+        b.x[i] = mx8_frag(p[0], p[4]);
         b.xs[i] = word(xs[i] + step * 4);  // the step's four blocks; a lane's own goes to byte 0 before use
       }
     };
@@ -122,13 +120,12 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
       const int left = g.K - whole * kMx8Step;
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bool in = h * 64 + kb * 16 < left;
-          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i] + (in ? static_cast<int64_t>(whole) * kMx8Step + h * 64 : -kb * 16));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) b.x[i].half[h][j] = in ? v[j] : 0u;
-        }
+        auto part = [&](int at) {
+          const bool in = at + kb * 16 < left;
+          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i] + (in ? static_cast<int64_t>(whole) * kMx8Step + at : -kb * 16));
+          return in ? v : mx8_u32x4{0u, 0u, 0u, 0u};
+        };
+        b.x[i] = mx8_frag(part(0), part(64));
         b.xs[i] = kb * 32 < left ? xs[i][whole * 4 + kb] : 0u;
       }
       multiply(b);

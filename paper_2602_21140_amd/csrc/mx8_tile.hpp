@@ -1,0 +1,302 @@
+// Product of microscaled 8-bit activations and weights for many rows: both operands through LDS.
+//
+// A workgroup of 8 wavefronts (2 x 4) computes 32 TM x 64 TN outputs (EPI8_H: half as many columns, gate and up of each), a
+// wavefront 16 TM x 16 TN, in steps of 128 K-elements.  Asynchronous copies bring a step's operands into one of two stages while
+// the step before is multiplied.
+//
+// A step goes through its row sub-tiles in pairs.  While a pair is multiplied the next one's activations are read from LDS; when
+// the last pair's are there, the stage is free: the workgroup meets at the step's one barrier, which publishes the next stage as
+// well, the copies of the step after that set out, and while the last pair is multiplied the next step's first fragments are read.
+//
+// LDS: weights lie in operand order, as in memory.  Activation row r is at r * 128 bytes, its 16-byte chunk c at chunk
+// c ^ ((r >> 1) & 7): a fragment read (16 rows, four chunks) meets no bank twice in any of its four passes.  A step's scales of
+// the weights come with them; those of the activations, whose rows may begin at any address, go through registers, three steps
+// ahead, into a ring of four.
+#pragma once
+
+#include "mx8_product.hpp"
+
+namespace revive {
+
+template <int TM, int TN>
+struct Mx8TileShape {
+  static constexpr int BM = 32 * TM, BN = 64 * TN, PANELS = BN / kMx8Panel;
+  static constexpr int STAGE_A = BM * kMx8Step, STAGE_B = BN * kMx8Step, STAGE_WS = PANELS * kMx8PanelScales, STAGE_XS = BM * 4;
+  static constexpr int B = 2 * STAGE_A, WS = B + 2 * STAGE_B, XS = WS + 2 * STAGE_WS;
+  static constexpr size_t LDS = XS + 4 * STAGE_XS;
+};
+
+template <int TM, int TN, int EPI>
+__global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
+  using S = Mx8TileShape<TM, TN>;
+  static_assert(TM % 2 == 0 && (TN == 2 || TN == 4) && (EPI != EPI8_H || TN == 4), "pairs of row sub-tiles, whole panels");
+  // K is two blocks at least, a row of A can be reached by 32 bits: the host sees to it.
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  typedef __attribute__((address_space(3))) void* lptr;
+  const bool dense = blockIdx.x < static_cast<unsigned>(a.dense.blocks);
+  const Mx8Problem g = dense ? a.dense : a.grouped;
+  const Mx8Tile t = mx8_tile_of(a, g, dense, S::BM);
+  if (t.row_begin >= t.row_end) return;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, kb = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const int KT = mx8_steps(g.K), k_blocks = g.K / kMx8Block;
+  const int rows = t.row_end - t.row_begin;
+
+  // ---- copies of a step: of A, BM / 8 rows per wavefront, 8 at a time; of B, an eighth of the panels; their scales, by wavefront 4
+  constexpr int CP_A = S::BM / 64, CP_B = S::STAGE_B / 8192;
+  auto source = [&](int r) -> int64_t {  // row of A; rows past the tile read its last row again
+    const int row = min(r, rows - 1);
+    return g.src_of ? g.src_of[t.row_begin + row] / g.k : row;
+  };
+  auto uniform64 = [](uint64_t v) {
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32)));
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
+    return (static_cast<uint64_t>(hi) << 32) | lo;
+  };
+  const int64_t first = g.src_of ? 0 : t.row_begin;  // the row that `source` counts from
+  const int left = g.K & (kMx8Step - 1);             // K-elements of a last step that is not whole
+  uint32_t a_off[CP_A];
+  auto a_chunk = [&](int i) { return (lane & 7) ^ swz(i * 8 + (lane >> 3)); };  // that copy i of A puts where the lane's 16 bytes go
+#pragma unroll
+  for (int i = 0; i < CP_A; ++i) a_off[i] = static_cast<uint32_t>(source((wave * CP_A + i) * 8 + (lane >> 3)) * g.a_row) + (a_chunk(i) << 4);
+  const int n_panels = (g.n_out + kMx8Panel - 1) / kMx8Panel;
+  auto matrix = [&](int p) {  // the workgroup's panel p
+    return EPI == EPI8_H ? t.n_idx : min(t.n_idx * S::PANELS + p, n_panels - 1);
+  };
+  constexpr int WAVES_A_PANEL = 8 / S::PANELS;
+  const int own_panel = wave / WAVES_A_PANEL;
+  uint64_t base_a = uniform64(reinterpret_cast<uint64_t>(g.A) + first * g.a_row);
+  uint64_t base_b = uniform64(reinterpret_cast<uint64_t>(t.B) + (EPI == EPI8_H && own_panel ? g.b_half : 0) +
+                              static_cast<int64_t>(matrix(own_panel)) * KT * kMx8PanelStep + (wave % WAVES_A_PANEL) * (CP_B * 1024));
+  uint64_t base_ws = uniform64(reinterpret_cast<uint64_t>(t.B) + g.b_codes);
+  // of the scales, lanes 0 to 31 take the first panel's, the others the second's
+  const uint32_t ws_off = static_cast<uint32_t>((lane >> 5) && S::PANELS > 1 ? (EPI == EPI8_H ? g.b_half : static_cast<int64_t>(matrix(1) - matrix(0)) * KT * kMx8PanelScales) : 0) + (lane & 31) * 16;
+  base_ws = uniform64(base_ws + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
+  // Five wait states before a copy may read a scalar register that a vector instruction wrote.
+  asm volatile("s_nop 4" : "+s"(base_a), "+s"(base_b), "+s"(base_ws));
+  const uint32_t lane16 = lane * 16;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lptr)smem));
+  auto to = [&](uint32_t at) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + at))); };
+  auto copy = [&](int kt, int stage) {
+    const uint64_t src_a = base_a + static_cast<uint64_t>(kt) * kMx8Step, src_b = base_b + static_cast<uint64_t>(kt) * kMx8PanelStep;
+    const int end = left && kt == KT - 1 ? left : kMx8Step;
+#pragma unroll
+    for (int i = 0; i < CP_A; ++i) {
+      // chunks past the row: the step's first one instead, cleared below
+      const uint32_t off = a_chunk(i) * 16 >= end ? a_off[i] - (a_chunk(i) << 4) : a_off[i];
+      copy_to_lds_16B(to(stage * S::STAGE_A + (wave * CP_A + i) * 1024), src_a, off);
+    }
+#pragma unroll
+    for (int i = 0; i < CP_B; ++i) copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), src_b + i * 1024, lane16);
+    if (wave == 4 && (S::PANELS == 2 || lane < 32)) copy_to_lds_16B(to(S::WS + stage * S::STAGE_WS), base_ws + static_cast<uint64_t>(kt) * kMx8PanelScales, ws_off);
+  };
+  // The last step's chunks past the row, of this wavefront's own copies, once these have landed.
+  auto clear_rest = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < CP_A; ++i)
+      if (a_chunk(i) * 16 >= left) *reinterpret_cast<mx8_u32x4*>(smem + stage * S::STAGE_A + (wave * CP_A + i) * 1024 + lane16) = mx8_u32x4{0u, 0u, 0u, 0u};
+  };
+
+  // ---- scales of the activations: of a step, BM rows of four bytes, a thread its part of a row; zeros past the row's end
+  constexpr int XB = S::STAGE_XS / 512;
+  typedef typename std::conditional<XB == 2, uint16_t, uint8_t>::type Part;
+  const uint8_t* xs_row = g.A_scales + (first + source(tid * XB / 4)) * k_blocks;
+  auto load_xs = [&](int kt) -> uint32_t {
+    typedef Part any __attribute__((aligned(1)));
+    const int at = min(kt * 4 + tid * XB % 4, k_blocks + 1), from = min(at, k_blocks - XB);
+    return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(xs_row + from))) >> (8 * (at - from));
+  };
+  auto store_xs = [&](int kt, uint32_t w) { *reinterpret_cast<Part*>(smem + S::XS + (kt & 3) * S::STAGE_XS + tid * XB) = static_cast<Part>(w); };
+
+  // ---- fragments: immediate offsets below 64 KiB from the lane's places
+  const unsigned char* fa0 = smem + (wm * 16 + r16) * 128 + ((kb ^ swz(r16)) << 4);        // first halves
+  const unsigned char* fa1 = smem + (wm * 16 + r16) * 128 + (((kb + 4) ^ swz(r16)) << 4);  // second halves
+  const unsigned char* fb = smem + S::B + (EPI == EPI8_H ? wn * 2 : wn * TN) * 2048 + lane16;
+  const unsigned char* fx = smem + S::XS + (wm * 16 + r16) * 4 + kb;
+  auto b_block = [](int tn) { return EPI == EPI8_H ? (tn >> 1) * 8 + (tn & 1) : tn; };
+  auto frag16 = [](const unsigned char* p) { return *reinterpret_cast<const mx8_u32x4*>(p); };
+  auto load_ws = [&](int stage) -> uint32_t {  // bytes: the scales of the wavefront's 16-row blocks
+    const unsigned char* p = smem + S::WS + stage * S::STAGE_WS + lane * 8;
+    if (EPI == EPI8_H) return *reinterpret_cast<const uint16_t*>(p + wn * 2) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + kMx8PanelScales + wn * 2)) << 16;
+    if (TN == 2) return *reinterpret_cast<const uint16_t*>(p + wn * 2);
+    return *reinterpret_cast<const uint32_t*>(p + (wn >> 1) * kMx8PanelScales + (wn & 1) * 4);
+  };
+  // 16-row sub-tiles are dealt round-robin to the two wavefront rows; pairs without a valid row are not multiplied
+  const int pairs = max(0, ((((rows + 15) >> 4) - wm + 1) / 2 + 1) / 2);
+
+  mx8_f32x4 acc[TM][TN];
+#pragma unroll
+  for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+    for (int tn = 0; tn < TN; ++tn) acc[tm][tn] = mx8_f32x4{0.f, 0.f, 0.f, 0.f};
+  // The pair's sums are made here: without this their products move down past the barriers, with all that they need.
+  auto pin = [&](auto q) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) {
+        mx8_f32x4& sum = acc[2 * q.value + i][tn];
+        asm volatile("" : "+v"(sum));
+      }
+  };
+
+  auto run = [&](auto q_tag) {
+    constexpr int Q = decltype(q_tag)::value;
+    Mx8Frag af[2][2], bf[TN];
+    uint32_t xs[2][2], ws = 0, xw = 0;
+    auto read_a = [&](int q, int stage, int kt, Mx8Frag* f, uint32_t* x) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        f[i] = mx8_frag(frag16(fa0 + stage * S::STAGE_A + (2 * q + i) * 4096), frag16(fa1 + stage * S::STAGE_A + (2 * q + i) * 4096));
+        x[i] = fx[(kt & 3) * S::STAGE_XS + (2 * q + i) * 128];
+      }
+    };
+    auto read_b = [&](int tn, int stage) {
+      const unsigned char* p = fb + stage * S::STAGE_B + b_block(tn) * 2048;
+      bf[tn] = mx8_frag(frag16(p), frag16(p + 1024));
+    };
+    // Step kt, in stage PH = kt % 2.
+    auto step = [&](int kt, auto ph_tag) {
+      constexpr int PH = decltype(ph_tag)::value;
+      constexpr int FLIP = (Q & 1) & PH;  // with an odd number of pairs the buffers change places from step to step
+      mx8_for_blocks<(Q > 0 ? Q - 1 : 0)>([&](auto q_at) {
+        constexpr int q = decltype(q_at)::value;
+        read_a(q + 1, PH, kt, af[(q + 1 + FLIP) & 1], xs[(q + 1 + FLIP) & 1]);
+        mx8_for_blocks<TN>([&](auto tn) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int f = (tn.value & 1) ? 1 - i : i;
+            acc[2 * q + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[(q + FLIP) & 1][f], acc[2 * q + f][tn.value], ws, xs[(q + FLIP) & 1][f]);
+          }
+        });
+        pin(q_at);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      if (left && kt + 1 == KT - 1) {
+        clear_rest(PH ^ 1);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      }
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      // everybody is done with this stage; the next one is there
+      store_xs(kt + 2, xw);  // read after the next barrier
+      xw = load_xs(kt + 3);
+      if (kt + 2 < KT) copy(kt + 2, PH);
+      __builtin_amdgcn_sched_barrier(0);
+      if (Q > 0) {
+        constexpr int LAST = (Q - 1 + FLIP) & 1;
+        read_a(0, PH ^ 1, kt + 1, af[LAST ^ 1], xs[LAST ^ 1]);
+        const uint32_t ws_next = load_ws(PH ^ 1);
+        mx8_for_blocks<TN>([&](auto tn) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int f = (tn.value & 1) ? 1 - i : i;
+            constexpr int M0 = Q > 0 ? 2 * (Q - 1) : 0;
+            acc[M0 + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[LAST][f], acc[M0 + f][tn.value], ws, xs[LAST][f]);
+          }
+          __builtin_amdgcn_sched_barrier(0);  // the registers of these weights take the next step's
+          read_b(tn.value, PH ^ 1);
+        });
+        pin(std::integral_constant<int, (Q > 0 ? Q - 1 : 0)>{});
+        ws = ws_next;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    xw = load_xs(2);
+    if (Q > 0) {
+      read_a(0, 0, 0, af[0], xs[0]);
+      ws = load_ws(0);
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) read_b(tn, 0);
+    }
+    int kt = 0;
+    for (; kt + 2 <= KT; kt += 2) {
+      step(kt, std::integral_constant<int, 0>{});
+      step(kt + 1, std::integral_constant<int, 1>{});
+    }
+    if (kt < KT) step(kt, std::integral_constant<int, 0>{});
+  };
+
+  copy(0, 0);
+  store_xs(0, load_xs(0));
+  store_xs(1, load_xs(1));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // the first step has landed
+  if (left && KT == 1) {
+    clear_rest(0);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+  }
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  if (KT > 1) copy(1, 1);
+  switch (pairs) {
+    case 0: run(std::integral_constant<int, 0>{}); break;
+    case 1: run(std::integral_constant<int, 1>{}); break;
+    case 2: run(std::integral_constant<int, 2>{}); break;
+    case 3: run(std::integral_constant<int, (TM > 4 ? 3 : 2)>{}); break;
+    default: run(std::integral_constant<int, TM / 2>{}); break;
+  }
+
+  // A lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16, in each set of 32 columns.  Results leave
+  // through LDS, by whole lines.
+  __syncthreads();  // the stages are free
+  if (EPI == EPI8_H) {
+    // the workgroup's rows of 128 bytes; 8-byte word w of row r at word w ^ (r & 15)
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      if (tm >= 2 * pairs) break;
+      const int row = (tm * 2 + wm) * 16 + r16, col = t.n_idx * kMx8Panel + wn * 32;
+      uint32_t byte;
+      const uint2 codes = mx8_swiglu_codes(acc[tm][0], acc[tm][1], acc[tm][TN > 2 ? 2 : 0], acc[tm][TN > 2 ? 3 : 0], byte);
+      *reinterpret_cast<uint2*>(smem + row * 128 + (((wn * 4 + kb) ^ r16) << 3)) = codes;
+      if (kb == 0 && row < rows && col < g.n_out) g.H_scales[static_cast<int64_t>(t.row_begin + row) * (g.n_out >> 5) + (col >> 5)] = static_cast<uint8_t>(byte);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < S::BM / 64; ++i) {  // eight neighbouring lanes: the 128 bytes of a row
+      const int row = i * 64 + (tid >> 3), w = (tid & 7) * 2, col = t.n_idx * kMx8Panel + w * 8;
+      const uint2 lo = *reinterpret_cast<const uint2*>(smem + row * 128 + ((w ^ (row & 15)) << 3));
+      const uint2 hi = *reinterpret_cast<const uint2*>(smem + row * 128 + (((w + 1) ^ (row & 15)) << 3));
+      if (row < rows && col < g.n_out) *reinterpret_cast<mx8_u32x4*>(g.H + static_cast<int64_t>(t.row_begin + row) * g.n_out + col) = mx8_u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  } else {
+    // 16 rows of 16 TN fp32 numbers at a time, in the wavefront's own part; 16-byte word w of row r at word w ^ r
+    unsigned char* out = smem + wave * (TN * 1024);
+    constexpr int LANES = 2 * TN, WORDS = 4 * TN;  // lanes to a row, with eight columns each; words of a row
+    const int r0 = lane / LANES, c = lane % LANES, col = t.n_idx * S::BN + wn * (16 * TN) + c * 8;
+    auto word = [&](int r, int w) { return reinterpret_cast<mx8_f32x4*>(out + r * (TN * 64) + ((w ^ (r & (WORDS - 1))) << 4)); };
+#pragma unroll
+    for (int tm = 0; tm < TM; ++tm) {
+      if (tm >= 2 * pairs) break;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn) *word(r16, (tn >> 1) * 8 + kb * 2 + (tn & 1)) = acc[tm][tn];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+      for (int r = r0; r < 16; r += 64 / LANES) {
+        const int row = (tm * 2 + wm) * 16 + r;
+        const mx8_f32x4 v0 = *word(r, 2 * c), v1 = *word(r, 2 * c + 1);
+        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        if (row >= rows) continue;
+        if (EPI == EPI8_LINEAR) mx8_store_linear(g, t.row_begin + row, col, v);
+        else if (col < g.n_out) mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(t.row_begin + row) * g.n_out, col, g.n_out, v);
+      }
+    }
+  }
+}
+
+template <int TM, int TN, int EPI>
+int launch_mx8_tile(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
+  const int grid = args.dense.blocks + args.grouped.blocks;
+  if (grid <= 0) return REVIVE_OK;
+  constexpr size_t lds = Mx8TileShape<TM, TN>::LDS;
+  auto kern = mx8_tile_kernel<TM, TN, EPI>;
+  REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(512), lds, stream, args);
+  return check_hip(ctx, hipGetLastError(), "mx8_tile launch");
+}
+
+}  // namespace revive
