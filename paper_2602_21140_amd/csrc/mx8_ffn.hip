@@ -74,15 +74,15 @@ int mx8_stream_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   Mx8Args a;
   if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 64, 256, a)) return too_large(ctx);
   KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
-  return launch_mx8_stream<TMX, 4, 4, EPI>(ctx, a, stream);
+  return launch_mx8_stream<TMX, 4, 4, 2, EPI>(ctx, a, stream);
 }
 
-template <int TM, int EPI>
+template <int EPI>
 int mx8_tile_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   Mx8Args a;
-  if (!mx8_args<EPI>(ctx, f, 32 * TM, EPI == EPI8_H ? 128 : 256, 512, a)) return too_large(ctx);
+  if (!mx8_args<EPI>(ctx, f, kMx8Tile, EPI == EPI8_H ? 128 : 256, 512, a)) return too_large(ctx);
   KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
-  return launch_mx8_tile<TM, 4, EPI>(ctx, a, stream);
+  return launch_mx8_tile<4, EPI>(ctx, a, stream);
 }
 
 }  // namespace
@@ -93,11 +93,11 @@ int launch_mx8_expert_ffn(revive_ctx* ctx, const uint8_t* x, const uint8_t* x_sc
   const Mx8Ffn f{x, x_scales, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * ctx->cfg.k, y_shared ? T : 0};
   // The tiles address a row of x by 32 bits.
   if (f.N > kMx8TileRowsPerSlot * static_cast<int64_t>(ctx->P) && static_cast<int64_t>(T) * ctx->cfg.H < (1ll << 32)) {
-    const int rc = mx8_tile_product<8, EPI8_H>(ctx, f, stream);
-    return rc != REVIVE_OK ? rc : mx8_tile_product<8, EPI8_Y>(ctx, f, stream);
+    const int rc = mx8_tile_product<EPI8_H>(ctx, f, stream);
+    return rc != REVIVE_OK ? rc : mx8_tile_product<EPI8_Y>(ctx, f, stream);
   }
-  const int rc = mx8_stream_product<4, EPI8_H>(ctx, f, stream);
-  return rc != REVIVE_OK ? rc : mx8_stream_product<4, EPI8_Y>(ctx, f, stream);
+  const int rc = mx8_stream_product<2, EPI8_H>(ctx, f, stream);
+  return rc != REVIVE_OK ? rc : mx8_stream_product<2, EPI8_Y>(ctx, f, stream);
 }
 
 }  // namespace revive

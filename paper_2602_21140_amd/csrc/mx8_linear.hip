@@ -10,20 +10,20 @@ namespace {
 
 int too_large() { return fail(nullptr, REVIVE_EINVAL, "revive_mx_eight_linear: rows times N is more than one launch takes"); }
 
-template <int TMX, int W, int NW>
+template <int TMX, int W, int NW, int D>
 int linear_stream(const Mx8Problem& base, hipStream_t stream) {
   Mx8Args a{};
   a.dense = base;
   if (!mx8_cut(a.dense, ceil_div(base.M, 16 * TMX), 16 * W, 64 * NW)) return too_large();
-  return launch_mx8_stream<TMX, W, NW, EPI8_LINEAR>(nullptr, a, stream);
+  return launch_mx8_stream<TMX, W, NW, D, EPI8_LINEAR>(nullptr, a, stream);
 }
 
-template <int TM, int TN>
+template <int TN>
 int linear_tile(const Mx8Problem& base, hipStream_t stream) {
   Mx8Args a{};
   a.dense = base;
-  if (!mx8_cut(a.dense, ceil_div(base.M, 32 * TM), 64 * TN, 512)) return too_large();
-  return launch_mx8_tile<TM, TN, EPI8_LINEAR>(nullptr, a, stream);
+  if (!mx8_cut(a.dense, ceil_div(base.M, kMx8Tile), 64 * TN, 512)) return too_large();
+  return launch_mx8_tile<TN, EPI8_LINEAR>(nullptr, a, stream);
 }
 
 }  // namespace
@@ -56,8 +56,8 @@ extern "C" int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales,
   p.activation = activation;
   p.n_out = N; p.K = K; p.M = rows;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (rows <= 16) return linear_stream<1, 2, 8>(p, s);
-  if (rows <= 128 || K < 64) return linear_stream<4, 4, 4>(p, s);  // the tiles take K from two blocks on
-  if (static_cast<int64_t>(rows) * N < 256 * 256 * 256) return linear_tile<4, 2>(p, s);
-  return linear_tile<8, 4>(p, s);
+  if (rows <= 16) return linear_stream<1, 2, 8, 2>(p, s);
+  if (rows <= 128 || K < 64) return linear_stream<2, 4, 4, 2>(p, s);  // the tiles take K from two blocks on
+  if (static_cast<int64_t>(rows) * N < 256 * 256 * 128) return linear_stream<2, 4, 4, 2>(p, s);
+  return linear_tile<4>(p, s);
 }

@@ -2,20 +2,30 @@
 //
 // A workgroup covers up to 16 TMX rows and W 16-row blocks of weight rows (EPI8_H: half of them gate, half up).  Its NW
 // wavefronts share K, each with a contiguous part of the steps of 128, and add up their sums through LDS at the end, in the
-// wavefronts' order.  So the K loop has no barrier and no LDS, and a product of few columns still has many wavefronts: what
-// bounds it is how fast HBM is read, and in the smallest calls latency.  Weights and activations of the next two steps are on
-// their way in registers.
+// wavefronts' order.  So the K loop has no barrier, and a product of few columns still has many wavefronts: what bounds it is how
+// fast HBM is read, and in the smallest calls latency.  Weights and activations of the next D steps are on their way in registers.
+//
+// How fast a CU's loads come goes by the lines that each touches.  Weights lie in the order in which the matrix cores want them;
+// of the activations a load takes whole lines, 8 rows of 128 bytes, and the wavefront turns them to operand order in LDS of its
+// own (as operands straight from memory, 16 rows of 64 bytes, a product of 64 rows takes twice as long).  Their scales come for
+// 16 steps at once.
 #pragma once
 
 #include "mx8_product.hpp"
 
 namespace revive {
 
-template <int TMX, int W, int NW, int EPI>
-constexpr size_t mx8_stream_lds() { return static_cast<size_t>(NW) * W * TMX * 1024; }
+constexpr int kMx8ScaleSteps = 16, kMx8ScaleRow = kMx8ScaleSteps + 1;  // words of a row's scales in LDS, and from row to row
+template <int TM>
+constexpr int mx8_stream_wave_lds() { return 16 * TM * (kMx8Step + 4 * kMx8ScaleRow); }  // a wavefront's activations and their scales
+template <int TMX, int W, int NW>
+constexpr size_t mx8_stream_lds() {
+  const int loop = NW * mx8_stream_wave_lds<TMX>(), sums = NW * W * TMX * 1024;
+  return loop > sums ? loop : sums;
+}
 
-template <int TMX, int W, int NW, int EPI>
-__global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
+template <int TMX, int W, int NW, int D, int EPI>
+__global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(Mx8Args a) {
   static_assert(W % 2 == 0 && W <= 4 && (EPI != EPI8_H || W == 4) && NW > 1, "output columns in sets of 32, sums by way of LDS");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const bool dense = blockIdx.x < static_cast<unsigned>(a.dense.blocks);
@@ -46,21 +56,26 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
   auto run = [&](auto tm_tag, auto once_tag) {
     constexpr int TM = decltype(tm_tag)::value;
     constexpr bool ONCE = decltype(once_tag)::value;  // streamed past the caches' retention (non-temporal)
-    const uint8_t* x[TM];
-    const uint8_t* xs[TM];
+    // load j of row-tile i: rows 16 i + 8 j + l / 8, chunk l % 8
+    const uint8_t* x[TM][2];
+    const uint8_t* xs[TM];  // rows 16 i + l / 4
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int64_t row = source(i * 16 + r16);
-      x[i] = g.A + row * g.a_row + kb * 16;
-      xs[i] = g.A_scales + row * blocks;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) x[i][j] = g.A + source(i * 16 + j * 8 + (lane >> 3)) * g.a_row + (lane & 7) * 16;
+      xs[i] = g.A_scales + source(i * 16 + (lane >> 2)) * blocks;
     }
+    unsigned char* own = smem + wave * mx8_stream_wave_lds<TM>();
+    uint32_t* own_scales = reinterpret_cast<uint32_t*>(own + 16 * TM * kMx8Step);
+    // row r at r * 128 bytes, its chunk c at chunk c ^ ((r >> 1) & 7)
+    auto place = [&](int row, int chunk) { return reinterpret_cast<mx8_u32x4*>(own + row * 128 + ((chunk ^ swz(row)) << 4)); };
     mx8_f32x4 acc[W][TM];
 #pragma unroll
     for (int s = 0; s < W; ++s)
 #pragma unroll
       for (int i = 0; i < TM; ++i) acc[s][i] = mx8_f32x4{0.f, 0.f, 0.f, 0.f};
 
-    struct Step { Mx8Frag w[W], x[TM]; uint32_t ws, xs[TM]; };
+    struct Step { Mx8Frag w[W]; uint32_t ws; mx8_u32x4 x[TM][2]; };
     auto word = [](const uint8_t* p) { typedef uint32_t any __attribute__((aligned(1))); return *reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(p)); };
     auto load_w = [&](Step& b, int step) {
 #pragma unroll
@@ -74,72 +89,84 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
       else if (W == 2) b.ws = two(scales[0]);
       else b.ws = word(scales[0] + at);
     };
-    auto multiply = [&](const Step& b) {
-      mx8_for_blocks<W>([&](auto s) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) acc[s.value][i] = mx8_mfma<s.value, 0>(b.w[s.value], b.x[i], acc[s.value][i], b.ws, b.xs[i]);
-      });
-    };
     auto load = [&](Step& b, int step) {  // a whole step
       load_w(b, step);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i] + static_cast<int64_t>(step) * kMx8Step));
-        b.x[i] = mx8_frag(p[0], p[4]);
-        b.xs[i] = word(xs[i] + step * 4);  // the step's four blocks; a lane's own goes to byte 0 before use
-      }
-    };
-    auto own_scales = [&](Step& b) {
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int i = 0; i < TM; ++i) b.xs[i] >>= kb * 8;
+        for (int j = 0; j < 2; ++j)
+          b.x[i][j] = *reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i][j] + static_cast<int64_t>(step) * kMx8Step));
+    };
+    auto multiply = [&](const Step& b, int at) {  // `at`: the step's place among the scales
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) *place(i * 16 + j * 8 + (lane >> 3), lane & 7) = b.x[i][j];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const Mx8Frag f = mx8_frag(*place(i * 16 + r16, kb), *place(i * 16 + r16, kb + 4));
+        const uint32_t scale = reinterpret_cast<const uint8_t*>(own_scales + (i * 16 + r16) * kMx8ScaleRow + at)[kb];
+        mx8_for_blocks<W>([&](auto s) { acc[s.value][i] = mx8_mfma<s.value, 0>(b.w[s.value], f, acc[s.value][i], b.ws, scale); });
+      }
     };
 
     const int whole = g.K / kMx8Step;
-    const int first = wave * whole / NW, last = (wave + 1) * whole / NW;  // KT < 2^18
-    if (first < last) {
-      Step b[2];
-      load(b[0], first);
-      load(b[1], min(first + 1, last - 1));
-      int s = first;
-      for (; s + 2 <= last; s += 2) {
+    const int begin = static_cast<int>(static_cast<int64_t>(wave) * whole / NW), end = static_cast<int>(static_cast<int64_t>(wave + 1) * whole / NW);
+    for (int first = begin; first < end; first += kMx8ScaleSteps) {
+      const int last = min(first + kMx8ScaleSteps, end);
+      uint32_t scale[TM][kMx8ScaleSteps / 4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          own_scales(b[u]);
-          multiply(b[u]);
-          load(b[u], min(s + u + 2, last - 1));  // past the last step that one again, not multiplied
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int p = 0; p < kMx8ScaleSteps / 4; ++p) scale[i][p] = word(xs[i] + min(first + 4 * p + (lane & 3), last - 1) * 4);
+      Step b[D];
+#pragma unroll
+      for (int u = 0; u < D; ++u)
+        if (first + u < last) load(b[u], first + u);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int p = 0; p < kMx8ScaleSteps / 4; ++p) own_scales[(i * 16 + (lane >> 2)) * kMx8ScaleRow + 4 * p + (lane & 3)] = scale[i][p];
+      int s = first;
+      for (; s + 2 * D <= last; s += D) {  // every load unconditional, so that the compiler's count of loads in flight stays exact
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+          multiply(b[u], s + u - first);
+          load(b[u], s + u + D);
         }
       }
-      if (s < last) {
-        own_scales(b[0]);
-        multiply(b[0]);
+#pragma unroll
+      for (int u = 0; u < 2 * D; ++u) {  // fewer than twice as many are left
+        if (s + u < last) multiply(b[u % D], s + u - first);
+        if (u < D && s + u + D < last) load(b[u % D], s + u + D);
       }
     }
     if (wave == NW - 1 && whole < KT) {  // what is left of K, a multiple of 32: zeros behind it, and scales of 2^-127
       Step b;
       load_w(b, whole);
       const int left = g.K - whole * kMx8Step;
+      const bool in = (lane & 7) * 16 < left;  // chunks past the row: its first one, not used
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        auto part = [&](int at) {
-          const bool in = at + kb * 16 < left;
-          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i] + (in ? static_cast<int64_t>(whole) * kMx8Step + at : -kb * 16));
-          return in ? v : mx8_u32x4{0u, 0u, 0u, 0u};
-        };
-        b.x[i] = mx8_frag(part(0), part(64));
-        b.xs[i] = kb * 32 < left ? xs[i][whole * 4 + kb] : 0u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i][j] + (in ? static_cast<int64_t>(whole) * kMx8Step : -(lane & 7) * 16));
+          b.x[i][j] = in ? v : mx8_u32x4{0u, 0u, 0u, 0u};
+        }
+        const int block = lane & 3;
+        reinterpret_cast<uint8_t*>(own_scales + (i * 16 + (lane >> 2)) * kMx8ScaleRow)[block] = block * 32 < left ? xs[i][whole * 4 + block] : 0;
       }
-      multiply(b);
+      multiply(b, 0);
     }
 
     // the wavefronts' sums, tile by tile; NW tiles at a time are added up, a wavefront each its own
     mx8_f32x4* part = reinterpret_cast<mx8_f32x4*>(smem);
-    if (NW > 1) {
+    __syncthreads();  // the activations are done with
 #pragma unroll
-      for (int s = 0; s < W; ++s)
+    for (int s = 0; s < W; ++s)
 #pragma unroll
-        for (int i = 0; i < TM; ++i) part[((wave * W + s) * TM + i) * 64 + lane] = acc[s][i];
-      __syncthreads();
-    }
+      for (int i = 0; i < TM; ++i) part[((wave * W + s) * TM + i) * 64 + lane] = acc[s][i];
+    __syncthreads();
     auto total = [&](int s, int i) {
       mx8_f32x4 v = part[(s * TM + i) * 64 + lane];
       for (int w = 1; w < NW; ++w) v += part[((w * W + s) * TM + i) * 64 + lane];
@@ -171,12 +198,12 @@ __global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
   else run(std::integral_constant<int, TMX>{}, Y{});
 }
 
-template <int TMX, int W, int NW, int EPI>
+template <int TMX, int W, int NW, int D, int EPI>
 int launch_mx8_stream(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
   const int grid = args.dense.blocks + args.grouped.blocks;
   if (grid <= 0) return REVIVE_OK;
-  constexpr size_t lds = mx8_stream_lds<TMX, W, NW, EPI>();
-  auto kern = mx8_stream_kernel<TMX, W, NW, EPI>;
+  constexpr size_t lds = mx8_stream_lds<TMX, W, NW>();
+  auto kern = mx8_stream_kernel<TMX, W, NW, D, EPI>;
   if (lds > 64 * 1024) REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
   hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * NW), lds, stream, args);
   return check_hip(ctx, hipGetLastError(), "mx8_stream launch");

@@ -1,35 +1,38 @@
 // Product of microscaled 8-bit activations and weights for many rows: both operands through LDS.
 //
-// A workgroup of 8 wavefronts (2 x 4) computes 32 TM x 64 TN outputs (EPI8_H: half as many columns, gate and up of each), a
-// wavefront 16 TM x 16 TN, in steps of 128 K-elements.  Asynchronous copies bring a step's operands into one of two stages while
-// the step before is multiplied.
+// A workgroup of 8 wavefronts (2 x 4) computes 256 x 64 TN outputs (EPI8_H: half as many columns, gate and up of each), a
+// wavefront 128 x 16 TN, in steps of 128 K-elements.  Asynchronous copies bring the steps' operands into two stages.
 //
-// A step goes through its row sub-tiles in pairs.  While a pair is multiplied the next one's activations are read from LDS; when
-// the last pair's are there, the stage is free: the workgroup meets at the step's one barrier, which publishes the next stage as
-// well, the copies of the step after that set out, and while the last pair is multiplied the next step's first fragments are read.
+// A step goes through its row sub-tiles in four pairs: while one is multiplied the next one's activations are read from LDS, and
+// during the last pair the next step's weights, all of them, and first activations.  So a stage is done with piece by piece, and
+// each piece is filled again at once, a step and a half before it is needed: at barrier X, after the first pair, the weights and
+// the activations of the first two pairs (everybody has read them), at barrier Y, after the third, those of the other two.  Each
+// barrier also publishes what was ordered a step and a half before; what was ordered since stays on its way.  With one barrier a
+// step, everything ordered at once, the copies and the products took turns.
 //
 // LDS: weights lie in operand order, as in memory.  Activation row r is at r * 128 bytes, its 16-byte chunk c at chunk
 // c ^ ((r >> 1) & 7): a fragment read (16 rows, four chunks) meets no bank twice in any of its four passes.  A step's scales of
-// the weights come with them; those of the activations, whose rows may begin at any address, go through registers, three steps
-// ahead, into a ring of four.
+// the weights come with them, those of the activations for four steps at a time.
 #pragma once
 
 #include "mx8_product.hpp"
 
 namespace revive {
 
-template <int TM, int TN>
+constexpr int kMx8Tile = 256;  // rows of a workgroup
+template <int TN>
 struct Mx8TileShape {
-  static constexpr int BM = 32 * TM, BN = 64 * TN, PANELS = BN / kMx8Panel;
-  static constexpr int STAGE_A = BM * kMx8Step, STAGE_B = BN * kMx8Step, STAGE_WS = PANELS * kMx8PanelScales, STAGE_XS = BM * 4;
+  static constexpr int TM = 8, BM = kMx8Tile, BN = 64 * TN, PANELS = BN / kMx8Panel;
+  static constexpr int STAGE_A = BM * kMx8Step, STAGE_B = BN * kMx8Step, STAGE_WS = PANELS * kMx8PanelScales, STAGE_XS = BM * 16;
   static constexpr int B = 2 * STAGE_A, WS = B + 2 * STAGE_B, XS = WS + 2 * STAGE_WS;
-  static constexpr size_t LDS = XS + 4 * STAGE_XS;
+  static constexpr size_t LDS = XS + 2 * STAGE_XS;
 };
 
-template <int TM, int TN, int EPI>
+template <int TN, int EPI>
 __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
-  using S = Mx8TileShape<TM, TN>;
-  static_assert(TM % 2 == 0 && (TN == 2 || TN == 4) && (EPI != EPI8_H || TN == 4), "pairs of row sub-tiles, whole panels");
+  using S = Mx8TileShape<TN>;
+  constexpr int TM = S::TM;
+  static_assert((TN == 2 || TN == 4) && (EPI != EPI8_H || TN == 4), "whole panels");
   // K is two blocks at least, a row of A can be reached by 32 bits: the host sees to it.
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   typedef __attribute__((address_space(3))) void* lptr;
@@ -43,8 +46,9 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   const int KT = mx8_steps(g.K), k_blocks = g.K / kMx8Block;
   const int rows = t.row_end - t.row_begin;
 
-  // ---- copies of a step: of A, BM / 8 rows per wavefront, 8 at a time; of B, an eighth of the panels; their scales, by wavefront 4
-  constexpr int CP_A = S::BM / 64, CP_B = S::STAGE_B / 8192;
+  // ---- copies of a step, by each wavefront: of either half of A's rows, 16, 8 at a time; of B, an eighth of the panels and of
+  // their scales
+  constexpr int CP_B = S::STAGE_B / 8192;
   auto source = [&](int r) -> int64_t {  // row of A; rows past the tile read its last row again
     const int row = min(r, rows - 1);
     return g.src_of ? g.src_of[t.row_begin + row] / g.k : row;
@@ -56,10 +60,12 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   };
   const int64_t first = g.src_of ? 0 : t.row_begin;  // the row that `source` counts from
   const int left = g.K & (kMx8Step - 1);             // K-elements of a last step that is not whole
-  uint32_t a_off[CP_A];
-  auto a_chunk = [&](int i) { return (lane & 7) ^ swz(i * 8 + (lane >> 3)); };  // that copy i of A puts where the lane's 16 bytes go
+  // copy i of A: rows 128 (i / 2) + 16 wave + 8 (i % 2) + l / 8
+  auto a_row = [&](int i) { return (i >> 1) * 128 + wave * 16 + (i & 1) * 8; };
+  auto a_chunk = [&](int i) { return (lane & 7) ^ swz((i & 1) * 8 + (lane >> 3)); };  // that the copy puts where the lane's 16 bytes go
+  uint32_t a_off[4];
 #pragma unroll
-  for (int i = 0; i < CP_A; ++i) a_off[i] = static_cast<uint32_t>(source((wave * CP_A + i) * 8 + (lane >> 3)) * g.a_row) + (a_chunk(i) << 4);
+  for (int i = 0; i < 4; ++i) a_off[i] = static_cast<uint32_t>(source(a_row(i) + (lane >> 3)) * g.a_row) + (a_chunk(i) << 4);
   const int n_panels = (g.n_out + kMx8Panel - 1) / kMx8Panel;
   auto matrix = [&](int p) {  // the workgroup's panel p
     return EPI == EPI8_H ? t.n_idx : min(t.n_idx * S::PANELS + p, n_panels - 1);
@@ -69,51 +75,72 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   uint64_t base_a = uniform64(reinterpret_cast<uint64_t>(g.A) + first * g.a_row);
   uint64_t base_b = uniform64(reinterpret_cast<uint64_t>(t.B) + (EPI == EPI8_H && own_panel ? g.b_half : 0) +
                               static_cast<int64_t>(matrix(own_panel)) * KT * kMx8PanelStep + (wave % WAVES_A_PANEL) * (CP_B * 1024));
-  uint64_t base_ws = uniform64(reinterpret_cast<uint64_t>(t.B) + g.b_codes);
-  // of the scales, lanes 0 to 31 take the first panel's, the others the second's
-  const uint32_t ws_off = static_cast<uint32_t>((lane >> 5) && S::PANELS > 1 ? (EPI == EPI8_H ? g.b_half : static_cast<int64_t>(matrix(1) - matrix(0)) * KT * kMx8PanelScales) : 0) + (lane & 31) * 16;
-  base_ws = uniform64(base_ws + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
+  // of the scales, lanes 0 to 31 take the first panel's, the others the second's; a wavefront 8 / PANELS of each
+  constexpr int WS_LANES = 4 * S::PANELS;
+  const int ws_lane = wave * WS_LANES + (lane & (WS_LANES - 1));
+  const uint32_t ws_off = static_cast<uint32_t>(ws_lane >= 32 ? (EPI == EPI8_H ? g.b_half : static_cast<int64_t>(matrix(1) - matrix(0)) * KT * kMx8PanelScales) : 0) + (ws_lane & 31) * 16;
+  uint64_t base_ws = uniform64(reinterpret_cast<uint64_t>(t.B) + g.b_codes + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
+  // the activations' scales of four steps, by copies where a row's words are words of memory
+  const bool xs_copied = (k_blocks & 3) == 0 && k_blocks >= 16 && (reinterpret_cast<uintptr_t>(g.A_scales) & 3) == 0;
+  const uint32_t xs_off = static_cast<uint32_t>(source(wave * 32 + (lane & 31)) * k_blocks);
+  uint64_t base_xs = uniform64(reinterpret_cast<uint64_t>(g.A_scales) + first * k_blocks);
   // Five wait states before a copy may read a scalar register that a vector instruction wrote.
-  asm volatile("s_nop 4" : "+s"(base_a), "+s"(base_b), "+s"(base_ws));
+  asm volatile("s_nop 4" : "+s"(base_a), "+s"(base_b), "+s"(base_ws), "+s"(base_xs));
   const uint32_t lane16 = lane * 16;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lptr)smem));
   auto to = [&](uint32_t at) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + at))); };
-  auto copy = [&](int kt, int stage) {
-    const uint64_t src_a = base_a + static_cast<uint64_t>(kt) * kMx8Step, src_b = base_b + static_cast<uint64_t>(kt) * kMx8PanelStep;
+  auto copy_a = [&](int kt, int stage, int half) {
+    const uint64_t src = base_a + static_cast<uint64_t>(kt) * kMx8Step;
     const int end = left && kt == KT - 1 ? left : kMx8Step;
 #pragma unroll
-    for (int i = 0; i < CP_A; ++i) {
+    for (int i = 2 * half; i < 2 * half + 2; ++i) {
       // chunks past the row: the step's first one instead, cleared below
       const uint32_t off = a_chunk(i) * 16 >= end ? a_off[i] - (a_chunk(i) << 4) : a_off[i];
-      copy_to_lds_16B(to(stage * S::STAGE_A + (wave * CP_A + i) * 1024), src_a, off);
+      copy_to_lds_16B(to(stage * S::STAGE_A + a_row(i) * 128), src, off);
     }
-#pragma unroll
-    for (int i = 0; i < CP_B; ++i) copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), src_b + i * 1024, lane16);
-    if (wave == 4 && (S::PANELS == 2 || lane < 32)) copy_to_lds_16B(to(S::WS + stage * S::STAGE_WS), base_ws + static_cast<uint64_t>(kt) * kMx8PanelScales, ws_off);
   };
+  auto copy_b = [&](int kt, int stage) {
+    const uint64_t src = base_b + static_cast<uint64_t>(kt) * kMx8PanelStep;
+#pragma unroll
+    for (int i = 0; i < CP_B; ++i) copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), src + i * 1024, lane16);
+    if (lane < WS_LANES) copy_to_lds_16B(to(S::WS + stage * S::STAGE_WS + wave * (WS_LANES * 16)), base_ws + static_cast<uint64_t>(kt) * kMx8PanelScales, ws_off);
+  };
+  constexpr int CP_X = 2 + CP_B + 1, CP_Y = 2;  // copies that a wavefront orders at either barrier
+  // Where group q (steps 4 q to 4 q + 3) of a row's scales is copied from: its words, or the row's last four.
+  auto xs_from = [&](int q) { return min(q * 16, max(k_blocks - 16, 0)); };
+  auto copy_xs = [&](int q) {
+    unsigned char* slot = smem + S::XS + (q & 1) * S::STAGE_XS;
+    if (xs_copied) {
+      if (lane < 32) copy_to_lds_16B(to(S::XS + (q & 1) * S::STAGE_XS + wave * 512), base_xs + xs_from(q), xs_off);
+    } else if (tid < S::BM) {  // byte by byte, zeros past the row's end; these loads are waited for here
+      const uint8_t* row = g.A_scales + (first + source(tid)) * k_blocks;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = q * 16 + w * 4 + i;
+          v |= (at < k_blocks ? static_cast<uint32_t>(row[min(at, k_blocks - 1)]) : 0u) << (8 * i);
+        }
+        *reinterpret_cast<uint32_t*>(slot + tid * 16 + w * 4) = v;
+      }
+    }
+  };
+  // Byte of a row's 16 where step kt's four scales are.
+  auto xs_at = [&](int kt) { return xs_copied ? kt * 4 - xs_from(kt >> 2) : (kt & 3) * 4; };
   // The last step's chunks past the row, of this wavefront's own copies, once these have landed.
-  auto clear_rest = [&](int stage) {
+  auto clear_rest = [&](int stage, int half) {
 #pragma unroll
-    for (int i = 0; i < CP_A; ++i)
-      if (a_chunk(i) * 16 >= left) *reinterpret_cast<mx8_u32x4*>(smem + stage * S::STAGE_A + (wave * CP_A + i) * 1024 + lane16) = mx8_u32x4{0u, 0u, 0u, 0u};
+    for (int i = 2 * half; i < 2 * half + 2; ++i)
+      if (a_chunk(i) * 16 >= left) *reinterpret_cast<mx8_u32x4*>(smem + stage * S::STAGE_A + a_row(i) * 128 + lane16) = mx8_u32x4{0u, 0u, 0u, 0u};
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(63));
   };
-
-  // ---- scales of the activations: of a step, BM rows of four bytes, a thread its part of a row; zeros past the row's end
-  constexpr int XB = S::STAGE_XS / 512;
-  typedef typename std::conditional<XB == 2, uint16_t, uint8_t>::type Part;
-  const uint8_t* xs_row = g.A_scales + (first + source(tid * XB / 4)) * k_blocks;
-  auto load_xs = [&](int kt) -> uint32_t {
-    typedef Part any __attribute__((aligned(1)));
-    const int at = min(kt * 4 + tid * XB % 4, k_blocks + 1), from = min(at, k_blocks - XB);
-    return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(xs_row + from))) >> (8 * (at - from));
-  };
-  auto store_xs = [&](int kt, uint32_t w) { *reinterpret_cast<Part*>(smem + S::XS + (kt & 3) * S::STAGE_XS + tid * XB) = static_cast<Part>(w); };
 
   // ---- fragments: immediate offsets below 64 KiB from the lane's places
   const unsigned char* fa0 = smem + (wm * 16 + r16) * 128 + ((kb ^ swz(r16)) << 4);        // first halves
   const unsigned char* fa1 = smem + (wm * 16 + r16) * 128 + (((kb + 4) ^ swz(r16)) << 4);  // second halves
   const unsigned char* fb = smem + S::B + (EPI == EPI8_H ? wn * 2 : wn * TN) * 2048 + lane16;
-  const unsigned char* fx = smem + S::XS + (wm * 16 + r16) * 4 + kb;
+  const unsigned char* fx = smem + S::XS + (wm * 16 + r16) * 16 + kb;
   auto b_block = [](int tn) { return EPI == EPI8_H ? (tn >> 1) * 8 + (tn & 1) : tn; };
   auto frag16 = [](const unsigned char* p) { return *reinterpret_cast<const mx8_u32x4*>(p); };
   auto load_ws = [&](int stage) -> uint32_t {  // bytes: the scales of the wavefront's 16-row blocks
@@ -144,12 +171,12 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   auto run = [&](auto q_tag) {
     constexpr int Q = decltype(q_tag)::value;
     Mx8Frag af[2][2], bf[TN];
-    uint32_t xs[2][2], ws = 0, xw = 0;
-    auto read_a = [&](int q, int stage, int kt, Mx8Frag* f, uint32_t* x) {
+    uint32_t xs[2][2], ws = 0;
+    auto read_a = [&](int q, int stage, int x_at, Mx8Frag* f, uint32_t* x) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f[i] = mx8_frag(frag16(fa0 + stage * S::STAGE_A + (2 * q + i) * 4096), frag16(fa1 + stage * S::STAGE_A + (2 * q + i) * 4096));
-        x[i] = fx[(kt & 3) * S::STAGE_XS + (2 * q + i) * 128];
+        x[i] = fx[x_at + (2 * q + i) * 512];
       }
     };
     auto read_b = [&](int tn, int stage) {
@@ -160,9 +187,10 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
     auto step = [&](int kt, auto ph_tag) {
       constexpr int PH = decltype(ph_tag)::value;
       constexpr int FLIP = (Q & 1) & PH;  // with an odd number of pairs the buffers change places from step to step
-      mx8_for_blocks<(Q > 0 ? Q - 1 : 0)>([&](auto q_at) {
+      const int x_at = ((kt >> 2) & 1) * S::STAGE_XS + xs_at(kt);
+      auto pair = [&](auto q_at) {  // multiply pair q, read the next one
         constexpr int q = decltype(q_at)::value;
-        read_a(q + 1, PH, kt, af[(q + 1 + FLIP) & 1], xs[(q + 1 + FLIP) & 1]);
+        read_a(q + 1, PH, x_at, af[(q + 1 + FLIP) & 1], xs[(q + 1 + FLIP) & 1]);
         mx8_for_blocks<TN>([&](auto tn) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -172,42 +200,50 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
         });
         pin(q_at);
         __builtin_amdgcn_sched_barrier(0);
-      });
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-      if (left && kt + 1 == KT - 1) {
-        clear_rest(PH ^ 1);
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      };
+      const bool more = kt + 2 < KT;
+      // All of this wavefront's copies but those of the last two barriers have landed, and its reads are done; then everybody's.
+      auto meet = [&](int clear_half) {
+        asm volatile("" ::: "memory");
+        if (more) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + CP_Y));
+        else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+        if (left && kt == KT - 1 - (clear_half ^ 1)) clear_rest((PH + (clear_half ^ 1)) & 1, clear_half);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      };
+      if constexpr (Q > 1) pair(std::integral_constant<int, 0>{});
+      meet(1);  // X: the second half of this step's rows is there
+      if ((kt & 3) == 0 && kt + 4 < KT) copy_xs((kt >> 2) + 1);
+      if (more) {
+        copy_a(kt + 2, PH, 0);
+        copy_b(kt + 2, PH);
       }
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      // everybody is done with this stage; the next one is there
-      store_xs(kt + 2, xw);  // read after the next barrier
-      xw = load_xs(kt + 3);
-      if (kt + 2 < KT) copy(kt + 2, PH);
       __builtin_amdgcn_sched_barrier(0);
-      if (Q > 0) {
+      if constexpr (Q > 2) pair(std::integral_constant<int, 1>{});
+      if constexpr (Q > 3) pair(std::integral_constant<int, 2>{});
+      meet(0);  // Y: the next step's weights and first half of rows are there
+      if (more) copy_a(kt + 2, PH, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (Q > 0) {
         constexpr int LAST = (Q - 1 + FLIP) & 1;
-        read_a(0, PH ^ 1, kt + 1, af[LAST ^ 1], xs[LAST ^ 1]);
+        read_a(0, PH ^ 1, (((kt + 1) >> 2) & 1) * S::STAGE_XS + xs_at(kt + 1), af[LAST ^ 1], xs[LAST ^ 1]);
         const uint32_t ws_next = load_ws(PH ^ 1);
         mx8_for_blocks<TN>([&](auto tn) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int f = (tn.value & 1) ? 1 - i : i;
-            constexpr int M0 = Q > 0 ? 2 * (Q - 1) : 0;
-            acc[M0 + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[LAST][f], acc[M0 + f][tn.value], ws, xs[LAST][f]);
+            acc[2 * (Q - 1) + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[LAST][f], acc[2 * (Q - 1) + f][tn.value], ws, xs[LAST][f]);
           }
           __builtin_amdgcn_sched_barrier(0);  // the registers of these weights take the next step's
           read_b(tn.value, PH ^ 1);
         });
-        pin(std::integral_constant<int, (Q > 0 ? Q - 1 : 0)>{});
+        pin(std::integral_constant<int, Q - 1>{});
         ws = ws_next;
       }
       __builtin_amdgcn_sched_barrier(0);
     };
-    xw = load_xs(2);
-    if (Q > 0) {
-      read_a(0, 0, 0, af[0], xs[0]);
+    if constexpr (Q > 0) {
+      read_a(0, 0, xs_at(0), af[0], xs[0]);
       ws = load_ws(0);
 #pragma unroll
       for (int tn = 0; tn < TN; ++tn) read_b(tn, 0);
@@ -220,24 +256,24 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
     if (kt < KT) step(kt, std::integral_constant<int, 0>{});
   };
 
-  copy(0, 0);
-  store_xs(0, load_xs(0));
-  store_xs(1, load_xs(1));
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // the first step has landed
-  if (left && KT == 1) {
-    clear_rest(0);
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+  copy_xs(0);
+  for (int kt = 0; kt < min(KT, 2); ++kt) {
+    copy_a(kt, kt, 0);
+    copy_b(kt, kt);
+    copy_a(kt, kt, 1);
   }
+  asm volatile("" ::: "memory");
+  if (KT > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + 2 * CP_Y));  // the first step's weights and first half have landed
+  else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+  if (left && KT == 1) clear_rest(0, 0);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  if (KT > 1) copy(1, 1);
   switch (pairs) {
     case 0: run(std::integral_constant<int, 0>{}); break;
     case 1: run(std::integral_constant<int, 1>{}); break;
     case 2: run(std::integral_constant<int, 2>{}); break;
-    case 3: run(std::integral_constant<int, (TM > 4 ? 3 : 2)>{}); break;
-    default: run(std::integral_constant<int, TM / 2>{}); break;
+    case 3: run(std::integral_constant<int, 3>{}); break;
+    default: run(std::integral_constant<int, 4>{}); break;
   }
 
   // A lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16, in each set of 32 columns.  Results leave
@@ -288,12 +324,12 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   }
 }
 
-template <int TM, int TN, int EPI>
+template <int TN, int EPI>
 int launch_mx8_tile(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
   const int grid = args.dense.blocks + args.grouped.blocks;
   if (grid <= 0) return REVIVE_OK;
-  constexpr size_t lds = Mx8TileShape<TM, TN>::LDS;
-  auto kern = mx8_tile_kernel<TM, TN, EPI>;
+  constexpr size_t lds = Mx8TileShape<TN>::LDS;
+  auto kern = mx8_tile_kernel<TN, EPI>;
   REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
   hipLaunchKernelGGL(kern, dim3(grid), dim3(512), lds, stream, args);
   return check_hip(ctx, hipGetLastError(), "mx8_tile launch");
