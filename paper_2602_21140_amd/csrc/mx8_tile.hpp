@@ -28,7 +28,14 @@ struct Mx8TileShape {
   static constexpr size_t LDS = XS + 2 * STAGE_XS;
 };
 
-template <int TN, int EPI>
+// Whether a product's rows of scales can be copied by words, four steps at a time.
+inline bool mx8_word_scales(const Mx8Problem& p) {
+  return p.K % kMx8Step == 0 && p.K >= 4 * kMx8Step && reinterpret_cast<uintptr_t>(p.A_scales) % 4 == 0;
+}
+
+// WORD_SCALES: both problems' are (mx8_word_scales).  Otherwise they go through registers, a step's at a time: loads that the
+// compiler waits for, and every copy with them, so that what was ordered since the last step does not stay on its way.
+template <int TN, int EPI, bool WORD_SCALES>
 __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   using S = Mx8TileShape<TN>;
   constexpr int TM = S::TM;
@@ -80,8 +87,6 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   const int ws_lane = wave * WS_LANES + (lane & (WS_LANES - 1));
   const uint32_t ws_off = static_cast<uint32_t>(ws_lane >= 32 ? (EPI == EPI8_H ? g.b_half : static_cast<int64_t>(matrix(1) - matrix(0)) * KT * kMx8PanelScales) : 0) + (ws_lane & 31) * 16;
   uint64_t base_ws = uniform64(reinterpret_cast<uint64_t>(t.B) + g.b_codes + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
-  // the activations' scales of four steps, by copies where a row's words are words of memory
-  const bool xs_copied = (k_blocks & 3) == 0 && k_blocks >= 16 && (reinterpret_cast<uintptr_t>(g.A_scales) & 3) == 0;
   const uint32_t xs_off = static_cast<uint32_t>(source(wave * 32 + (lane & 31)) * k_blocks);
   uint64_t base_xs = uniform64(reinterpret_cast<uint64_t>(g.A_scales) + first * k_blocks);
   // Five wait states before a copy may read a scalar register that a vector instruction wrote.
@@ -89,45 +94,43 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   const uint32_t lane16 = lane * 16;
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lptr)smem));
   auto to = [&](uint32_t at) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + at))); };
-  auto copy_a = [&](int kt, int stage, int half) {
-    const uint64_t src = base_a + static_cast<uint64_t>(kt) * kMx8Step;
+  // Copy i of A (0, 1: of the first half of the rows), copy i of B, a step's scales of B.
+  auto copy_a = [&](int kt, int stage, int i) {
+    // chunks past the row: the step's first one instead, cleared below
     const int end = left && kt == KT - 1 ? left : kMx8Step;
-#pragma unroll
-    for (int i = 2 * half; i < 2 * half + 2; ++i) {
-      // chunks past the row: the step's first one instead, cleared below
-      const uint32_t off = a_chunk(i) * 16 >= end ? a_off[i] - (a_chunk(i) << 4) : a_off[i];
-      copy_to_lds_16B(to(stage * S::STAGE_A + a_row(i) * 128), src, off);
-    }
+    const uint32_t off = a_chunk(i) * 16 >= end ? a_off[i] - (a_chunk(i) << 4) : a_off[i];
+    copy_to_lds_16B(to(stage * S::STAGE_A + a_row(i) * 128), base_a + static_cast<uint64_t>(kt) * kMx8Step, off);
   };
-  auto copy_b = [&](int kt, int stage) {
-    const uint64_t src = base_b + static_cast<uint64_t>(kt) * kMx8PanelStep;
-#pragma unroll
-    for (int i = 0; i < CP_B; ++i) copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), src + i * 1024, lane16);
+  auto copy_b = [&](int kt, int stage, int i) {
+    copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), base_b + static_cast<uint64_t>(kt) * kMx8PanelStep + i * 1024, lane16);
+  };
+  auto copy_ws = [&](int kt, int stage) {
     if (lane < WS_LANES) copy_to_lds_16B(to(S::WS + stage * S::STAGE_WS + wave * (WS_LANES * 16)), base_ws + static_cast<uint64_t>(kt) * kMx8PanelScales, ws_off);
   };
-  constexpr int CP_X = 2 + CP_B + 1, CP_Y = 2;  // copies that a wavefront orders at either barrier
-  // Where group q (steps 4 q to 4 q + 3) of a row's scales is copied from: its words, or the row's last four.
-  auto xs_from = [&](int q) { return min(q * 16, max(k_blocks - 16, 0)); };
-  auto copy_xs = [&](int q) {
-    unsigned char* slot = smem + S::XS + (q & 1) * S::STAGE_XS;
-    if (xs_copied) {
-      if (lane < 32) copy_to_lds_16B(to(S::XS + (q & 1) * S::STAGE_XS + wave * 512), base_xs + xs_from(q), xs_off);
-    } else if (tid < S::BM) {  // byte by byte, zeros past the row's end; these loads are waited for here
-      const uint8_t* row = g.A_scales + (first + source(tid)) * k_blocks;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t v = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = q * 16 + w * 4 + i;
-          v |= (at < k_blocks ? static_cast<uint32_t>(row[min(at, k_blocks - 1)]) : 0u) << (8 * i);
-        }
-        *reinterpret_cast<uint32_t*>(slot + tid * 16 + w * 4) = v;
-      }
-    }
+  constexpr int CP_X = 2 + CP_B + 1, CP_Y = 2;  // copies that a wavefront orders after either barrier
+  auto copy_x = [&](int kt, int stage, int n) {  // number n of X's
+    if (n < 2) copy_a(kt, stage, n);
+    else if (n < 2 + CP_B) copy_b(kt, stage, n - 2);
+    else if (n < CP_X) copy_ws(kt, stage);
   };
-  // Byte of a row's 16 where step kt's four scales are.
-  auto xs_at = [&](int kt) { return xs_copied ? kt * 4 - xs_from(kt >> 2) : (kt & 3) * 4; };
+  auto copy_y = [&](int kt, int stage, int n) { copy_a(kt, stage, 2 + n); };
+  // ---- scales of the activations.  WORD_SCALES: group q (steps 4 q to 4 q + 3), 16 bytes a row, in one of two places; the last
+  // group is the row's last 16 bytes.
+  auto xs_from = [&](int q) { return min(q * 16, k_blocks - 16); };
+  auto copy_xs = [&](int q) {
+    if (lane < 32) copy_to_lds_16B(to(S::XS + (q & 1) * S::STAGE_XS + wave * 512), base_xs + xs_from(q), xs_off);
+  };
+  // Otherwise: a thread half of a row's four bytes of a step, zeros past the row's end, in one of four places.
+  const uint8_t* xs_row = g.A_scales + (first + source(tid >> 1)) * k_blocks;
+  auto load_xs = [&](int kt) -> uint32_t {
+    typedef uint16_t any __attribute__((aligned(1)));
+    const int at = min(kt * 4 + (tid & 1) * 2, k_blocks + 1), from = min(at, k_blocks - 2);
+    return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(xs_row + from))) >> (8 * (at - from));
+  };
+  auto store_xs = [&](int kt, uint32_t w) { *reinterpret_cast<uint16_t*>(smem + S::XS + (kt & 3) * (S::STAGE_XS / 4) + tid * 2) = static_cast<uint16_t>(w); };
+  // Where step kt's four scales are, from row 0's first.
+  constexpr int XS_ROW = WORD_SCALES ? 16 : 4;
+  auto xs_at = [&](int kt) { return WORD_SCALES ? ((kt >> 2) & 1) * S::STAGE_XS + kt * 4 - xs_from(kt >> 2) : (kt & 3) * (S::STAGE_XS / 4); };
   // The last step's chunks past the row, of this wavefront's own copies, once these have landed.
   auto clear_rest = [&](int stage, int half) {
 #pragma unroll
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   const unsigned char* fa0 = smem + (wm * 16 + r16) * 128 + ((kb ^ swz(r16)) << 4);        // first halves
   const unsigned char* fa1 = smem + (wm * 16 + r16) * 128 + (((kb + 4) ^ swz(r16)) << 4);  // second halves
   const unsigned char* fb = smem + S::B + (EPI == EPI8_H ? wn * 2 : wn * TN) * 2048 + lane16;
-  const unsigned char* fx = smem + S::XS + (wm * 16 + r16) * 16 + kb;
+  const unsigned char* fx = smem + S::XS + (wm * 16 + r16) * XS_ROW + kb;
   auto b_block = [](int tn) { return EPI == EPI8_H ? (tn >> 1) * 8 + (tn & 1) : tn; };
   auto frag16 = [](const unsigned char* p) { return *reinterpret_cast<const mx8_u32x4*>(p); };
   auto load_ws = [&](int stage) -> uint32_t {  // bytes: the scales of the wavefront's 16-row blocks
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
     if (TN == 2) return *reinterpret_cast<const uint16_t*>(p + wn * 2);
     return *reinterpret_cast<const uint32_t*>(p + (wn >> 1) * kMx8PanelScales + (wn & 1) * 4);
   };
-  // 16-row sub-tiles are dealt round-robin to the two wavefront rows; pairs without a valid row are not multiplied
+  // 16-row sub-tiles are dealt round-robin to the two wavefront rows; of the four pairs none, two or all are multiplied
   const int pairs = max(0, ((((rows + 15) >> 4) - wm + 1) / 2 + 1) / 2);
 
   mx8_f32x4 acc[TM][TN];
@@ -169,79 +172,95 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   };
 
   auto run = [&](auto q_tag) {
-    constexpr int Q = decltype(q_tag)::value;
+    constexpr int Q = decltype(q_tag)::value;  // even: a step ends with the second buffer of activations, and the next one begins with the first
     Mx8Frag af[2][2], bf[TN];
-    uint32_t xs[2][2], ws = 0;
+    uint32_t xs[2][2], ws = 0, xw = 0;
     auto read_a = [&](int q, int stage, int x_at, Mx8Frag* f, uint32_t* x) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         f[i] = mx8_frag(frag16(fa0 + stage * S::STAGE_A + (2 * q + i) * 4096), frag16(fa1 + stage * S::STAGE_A + (2 * q + i) * 4096));
-        x[i] = fx[x_at + (2 * q + i) * 512];
+        x[i] = fx[x_at + (2 * q + i) * (32 * XS_ROW)];
       }
     };
     auto read_b = [&](int tn, int stage) {
       const unsigned char* p = fb + stage * S::STAGE_B + b_block(tn) * 2048;
       bf[tn] = mx8_frag(frag16(p), frag16(p + 1024));
     };
-    // Step kt, in stage PH = kt % 2.
-    auto step = [&](int kt, auto ph_tag) {
-      constexpr int PH = decltype(ph_tag)::value;
-      constexpr int FLIP = (Q & 1) & PH;  // with an odd number of pairs the buffers change places from step to step
-      const int x_at = ((kt >> 2) & 1) * S::STAGE_XS + xs_at(kt);
-      auto pair = [&](auto q_at) {  // multiply pair q, read the next one
+    // Step kt, in stage kt % 2; MORE: there are two steps behind it.  Copies go out one at a time between the products: ordered
+    // all at once behind the barrier they held the wavefronts up.
+    auto step = [&](int kt, auto more_tag) {
+      const int now = kt & 1, next = now ^ 1;
+      constexpr bool MORE = decltype(more_tag)::value;
+      const int x_at = xs_at(kt);
+      auto pair = [&](auto q_at, auto between) {  // multiply pair q, read the next one
         constexpr int q = decltype(q_at)::value;
-        read_a(q + 1, PH, x_at, af[(q + 1 + FLIP) & 1], xs[(q + 1 + FLIP) & 1]);
+        read_a(q + 1, now, x_at, af[(q + 1) & 1], xs[(q + 1) & 1]);
         mx8_for_blocks<TN>([&](auto tn) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int f = (tn.value & 1) ? 1 - i : i;
-            acc[2 * q + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[(q + FLIP) & 1][f], acc[2 * q + f][tn.value], ws, xs[(q + FLIP) & 1][f]);
+            acc[2 * q + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[q & 1][f], acc[2 * q + f][tn.value], ws, xs[q & 1][f]);
           }
+          between(tn.value);
         });
         pin(q_at);
         __builtin_amdgcn_sched_barrier(0);
       };
-      const bool more = kt + 2 < KT;
-      // All of this wavefront's copies but those of the last two barriers have landed, and its reads are done; then everybody's.
+      // All of this wavefront's copies but those since the barrier before the last have landed, and its reads are done; then
+      // everybody's.
       auto meet = [&](int clear_half) {
         asm volatile("" ::: "memory");
-        if (more) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + CP_Y));
-        else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-        if (left && kt == KT - 1 - (clear_half ^ 1)) clear_rest((PH + (clear_half ^ 1)) & 1, clear_half);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(MORE ? CP_X + CP_Y : 0));
+        if (!MORE && left && kt == KT - 1 - (clear_half ^ 1)) clear_rest(clear_half ? now : next, clear_half);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       };
-      if constexpr (Q > 1) pair(std::integral_constant<int, 0>{});
+      auto nothing = [](int) {};
+      // n copies of `copy` from number `from` on
+      auto copies = [&](auto copy, int from, int n) {
+        if (!MORE) return;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < n; ++i) copy(kt + 2, now, from + i);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      if constexpr (Q > 0) pair(std::integral_constant<int, 0>{}, nothing);
       meet(1);  // X: the second half of this step's rows is there
-      if ((kt & 3) == 0 && kt + 4 < KT) copy_xs((kt >> 2) + 1);
-      if (more) {
-        copy_a(kt + 2, PH, 0);
-        copy_b(kt + 2, PH);
+      if (WORD_SCALES) {
+        if ((kt & 3) == 0 && kt + 4 < KT) copy_xs((kt >> 2) + 1);
+      } else {
+        store_xs(kt + 2, xw);  // read after the next barriers
+        xw = load_xs(kt + 3);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (Q > 2) pair(std::integral_constant<int, 1>{});
-      if constexpr (Q > 3) pair(std::integral_constant<int, 2>{});
+      if constexpr (Q == 4) {
+        constexpr int EACH = (CP_X + 2 * TN - 1) / (2 * TN);
+        pair(std::integral_constant<int, 1>{}, [&](int tn) { copies(copy_x, tn * EACH, EACH); });
+        pair(std::integral_constant<int, 2>{}, [&](int tn) { copies(copy_x, (TN + tn) * EACH, EACH); });
+      } else {
+        copies(copy_x, 0, CP_X);
+      }
       meet(0);  // Y: the next step's weights and first half of rows are there
-      if (more) copy_a(kt + 2, PH, 1);
-      __builtin_amdgcn_sched_barrier(0);
       if constexpr (Q > 0) {
-        constexpr int LAST = (Q - 1 + FLIP) & 1;
-        read_a(0, PH ^ 1, (((kt + 1) >> 2) & 1) * S::STAGE_XS + xs_at(kt + 1), af[LAST ^ 1], xs[LAST ^ 1]);
-        const uint32_t ws_next = load_ws(PH ^ 1);
+        read_a(0, next, xs_at(kt + 1), af[0], xs[0]);
+        const uint32_t ws_next = load_ws(next);
         mx8_for_blocks<TN>([&](auto tn) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int f = (tn.value & 1) ? 1 - i : i;
-            acc[2 * (Q - 1) + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[LAST][f], acc[2 * (Q - 1) + f][tn.value], ws, xs[LAST][f]);
+            acc[2 * (Q - 1) + f][tn.value] = mx8_mfma<tn.value, 0>(bf[tn.value], af[1][f], acc[2 * (Q - 1) + f][tn.value], ws, xs[1][f]);
           }
           __builtin_amdgcn_sched_barrier(0);  // the registers of these weights take the next step's
-          read_b(tn.value, PH ^ 1);
+          read_b(tn.value, next);
+          if (tn.value < CP_Y) copies(copy_y, tn.value, 1);
         });
         pin(std::integral_constant<int, Q - 1>{});
         ws = ws_next;
+      } else {
+        copies(copy_y, 0, CP_Y);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
+    if (!WORD_SCALES) xw = load_xs(2);
     if constexpr (Q > 0) {
       read_a(0, 0, xs_at(0), af[0], xs[0]);
       ws = load_ws(0);
@@ -249,18 +268,21 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
       for (int tn = 0; tn < TN; ++tn) read_b(tn, 0);
     }
     int kt = 0;
-    for (; kt + 2 <= KT; kt += 2) {
-      step(kt, std::integral_constant<int, 0>{});
-      step(kt + 1, std::integral_constant<int, 1>{});
-    }
-    if (kt < KT) step(kt, std::integral_constant<int, 0>{});
+    for (; kt + 2 < KT; ++kt) step(kt, std::true_type{});
+    for (; kt < KT; ++kt) step(kt, std::false_type{});
   };
 
-  copy_xs(0);
+  if (WORD_SCALES) {
+    copy_xs(0);
+  } else {
+    store_xs(0, load_xs(0));
+    store_xs(1, load_xs(1));
+  }
   for (int kt = 0; kt < min(KT, 2); ++kt) {
-    copy_a(kt, kt, 0);
-    copy_b(kt, kt);
-    copy_a(kt, kt, 1);
+#pragma unroll
+    for (int n = 0; n < CP_X; ++n) copy_x(kt, kt, n);
+#pragma unroll
+    for (int n = 0; n < CP_Y; ++n) copy_y(kt, kt, n);
   }
   asm volatile("" ::: "memory");
   if (KT > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + 2 * CP_Y));  // the first step's weights and first half have landed
@@ -268,13 +290,9 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   if (left && KT == 1) clear_rest(0, 0);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  switch (pairs) {
-    case 0: run(std::integral_constant<int, 0>{}); break;
-    case 1: run(std::integral_constant<int, 1>{}); break;
-    case 2: run(std::integral_constant<int, 2>{}); break;
-    case 3: run(std::integral_constant<int, 3>{}); break;
-    default: run(std::integral_constant<int, 4>{}); break;
-  }
+  if (pairs > 2) run(std::integral_constant<int, 4>{});
+  else if (pairs > 0) run(std::integral_constant<int, 2>{});
+  else run(std::integral_constant<int, 0>{});
 
   // A lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16, in each set of 32 columns.  Results leave
   // through LDS, by whole lines.
@@ -301,38 +319,98 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   } else {
     // 16 rows of 16 TN fp32 numbers at a time, in the wavefront's own part; 16-byte word w of row r at word w ^ r
     unsigned char* out = smem + wave * (TN * 1024);
-    constexpr int LANES = 2 * TN, WORDS = 4 * TN;  // lanes to a row, with eight columns each; words of a row
-    const int r0 = lane / LANES, c = lane % LANES, col = t.n_idx * S::BN + wn * (16 * TN) + c * 8;
+    constexpr int LANES = 2 * TN, WORDS = 4 * TN, COLS = 16 * TN;  // lanes to a row, with eight columns each; words, columns of a row
+    constexpr int TURNS = 16 * LANES / 64;
+    const int r0 = lane / LANES, c = lane % LANES, col0 = t.n_idx * S::BN + wn * COLS, col = col0 + c * 8;
     auto word = [&](int r, int w) { return reinterpret_cast<mx8_f32x4*>(out + r * (TN * 64) + ((w ^ (r & (WORDS - 1))) << 4)); };
+    const bool whole = col + 8 <= g.n_out;
+    if (EPI == EPI8_LINEAR) {
+      // all of the residual at once, so that its latency shows once
+      mx8_u32x4 res[TM][TURNS];
+      if (g.residual) {
 #pragma unroll
-    for (int tm = 0; tm < TM; ++tm) {
-      if (tm >= 2 * pairs) break;
-      __builtin_amdgcn_wave_barrier();
+        for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
-      for (int tn = 0; tn < TN; ++tn) *word(r16, (tn >> 1) * 8 + kb * 2 + (tn & 1)) = acc[tm][tn];
-      __builtin_amdgcn_wave_barrier();
+          for (int i = 0; i < TURNS; ++i) {
+            const int row = min((tm * 2 + wm) * 16 + i * (64 / LANES) + r0, rows - 1);
+            res[tm][i] = whole ? mx8_load_any<false>(g.residual + (t.row_begin + row) * g.ld_residual + col) : mx8_u32x4{0u, 0u, 0u, 0u};
+          }
+      }
+      uint32_t bias[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      const bool plain = g.activation == REVIVE_ACT_NONE;
+      if (g.bias && plain) mx8_load8<float, false>(g.bias, col, g.n_out, bias);
+      const int own_col = col0 + lane % COLS;
+      const float own_bias = g.bias && own_col < g.n_out ? g.bias[own_col] : 0.f;
+#pragma unroll
+      for (int tm = 0; tm < TM; ++tm) {
+        if (tm >= 2 * pairs) break;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn) *word(r16, (tn >> 1) * 8 + kb * 2 + (tn & 1)) = acc[tm][tn];
+        __builtin_amdgcn_wave_barrier();
+        if (!plain) {  // a lane its column, number by number
 #pragma unroll 1
-      for (int r = r0; r < 16; r += 64 / LANES) {
-        const int row = (tm * 2 + wm) * 16 + r;
-        const mx8_f32x4 v0 = *word(r, 2 * c), v1 = *word(r, 2 * c + 1);
-        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-        if (row >= rows) continue;
-        if (EPI == EPI8_LINEAR) mx8_store_linear(g, t.row_begin + row, col, v);
-        else if (col < g.n_out) mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(t.row_begin + row) * g.n_out, col, g.n_out, v);
+          for (int r = lane / COLS; r < 16; r += 64 / COLS) {
+            float* v = reinterpret_cast<float*>(word(r, (lane % COLS) >> 2)) + (lane & 3);
+            *v = mx8_activated(*v + own_bias, g.activation);
+          }
+          __builtin_amdgcn_wave_barrier();
+        }
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+          const int r = i * (64 / LANES) + r0, row = (tm * 2 + wm) * 16 + r;
+          const mx8_f32x4 v0 = *word(r, 2 * c), v1 = *word(r, 2 * c + 1);
+          float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+          if (row >= rows) continue;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(bias[j]);
+          if (g.residual) {
+            uint32_t bits[8];
+            if (whole) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) bits[j] = (j & 1) ? res[tm][i][j / 2] & 0xFFFF0000u : res[tm][i][j / 2] << 16;
+            } else {
+              mx8_load8<uint16_t, false>(g.residual + (t.row_begin + row) * g.ld_residual, col, g.n_out, bits);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(bits[j]);
+          }
+          mx8_store8<uint16_t, false>(g.Y + (t.row_begin + row) * g.ldy, col, g.n_out, v);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int tm = 0; tm < TM; ++tm) {
+        if (tm >= 2 * pairs) break;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn) *word(r16, (tn >> 1) * 8 + kb * 2 + (tn & 1)) = acc[tm][tn];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+          const int r = i * (64 / LANES) + r0, row = (tm * 2 + wm) * 16 + r;
+          const mx8_f32x4 v0 = *word(r, 2 * c), v1 = *word(r, 2 * c + 1);
+          const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+          if (row < rows && whole) mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(t.row_begin + row) * g.n_out, col, g.n_out, v);
+        }
       }
     }
   }
 }
 
+template <int TN, int EPI, bool WORD_SCALES>
+int launch_mx8_tile_as(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
+  constexpr size_t lds = Mx8TileShape<TN>::LDS;
+  auto kern = mx8_tile_kernel<TN, EPI, WORD_SCALES>;
+  REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
+  hipLaunchKernelGGL(kern, dim3(args.dense.blocks + args.grouped.blocks), dim3(512), lds, stream, args);
+  return check_hip(ctx, hipGetLastError(), "mx8_tile launch");
+}
 template <int TN, int EPI>
 int launch_mx8_tile(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
-  const int grid = args.dense.blocks + args.grouped.blocks;
-  if (grid <= 0) return REVIVE_OK;
-  constexpr size_t lds = Mx8TileShape<TN>::LDS;
-  auto kern = mx8_tile_kernel<TN, EPI>;
-  REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(512), lds, stream, args);
-  return check_hip(ctx, hipGetLastError(), "mx8_tile launch");
+  if (args.dense.blocks + args.grouped.blocks <= 0) return REVIVE_OK;
+  const bool words = (args.dense.blocks == 0 || mx8_word_scales(args.dense)) && (args.grouped.blocks == 0 || mx8_word_scales(args.grouped));
+  return words ? launch_mx8_tile_as<TN, EPI, true>(ctx, args, stream) : launch_mx8_tile_as<TN, EPI, false>(ctx, args, stream);
 }
 
 }  // namespace revive
