@@ -14,7 +14,7 @@ namespace revive {
 
 namespace {
 
-constexpr int kMx8TileRowsPerSlot = 48;
+constexpr int kMx8TileRowsPerSlot = 24, kMx8TileGrid = 96;
 
 struct Mx8Ffn {
   const uint8_t* x; const uint8_t* x_scales;
@@ -69,20 +69,32 @@ bool mx8_args(const revive_ctx* ctx, const Mx8Ffn& f, int tile_m, int width, int
 
 int too_large(const revive_ctx* ctx) { return fail(ctx, REVIVE_EINVAL, "revive_mx_eight_expert_ffn: rows times columns are more than one launch takes"); }
 
-template <int TMX, int EPI>
+template <int TMX, int W, int D, int EPI, bool WIDE = false>
 int mx8_stream_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   Mx8Args a;
-  if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 64, 256, a)) return too_large(ctx);
-  KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
-  return launch_mx8_stream<TMX, 4, 4, 2, EPI>(ctx, a, stream);
+  if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 16 * W, 256, a)) return too_large(ctx);
+  return launch_mx8_stream<TMX, W, 4, D, EPI, WIDE>(ctx, a, stream);
 }
 
 template <int EPI>
 int mx8_tile_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   Mx8Args a;
   if (!mx8_args<EPI>(ctx, f, kMx8Tile, EPI == EPI8_H ? 128 : 256, 512, a)) return too_large(ctx);
-  KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
   return launch_mx8_tile<4, EPI>(ctx, a, stream);
+}
+
+// One of the two products, in the form that suits its rows.
+template <int EPI>
+int mx8_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
+  KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
+  const revive_config& c = ctx->cfg;
+  // All of x within 32 bits, as the tiles and the narrow form of the stream address it.
+  const bool wide = EPI == EPI8_H && static_cast<int64_t>(ctx->cfg.T_max) * c.H >= (1ll << 32);
+  if (wide) return mx8_stream_product<2, 4, 2, EPI, EPI == EPI8_H>(ctx, f, stream);
+  if (f.N <= kMx8TileRowsPerSlot * static_cast<int64_t>(ctx->P)) return mx8_stream_product<2, 4, 2, EPI>(ctx, f, stream);
+  const int columns = EPI == EPI8_H ? ceil_div(c.I, 128) : ceil_div(c.H, 256);
+  if (static_cast<int64_t>(std::max(ctx->P, f.N / kMx8Tile)) * columns >= kMx8TileGrid) return mx8_tile_product<EPI>(ctx, f, stream);
+  return mx8_stream_product<4, 4, 1, EPI>(ctx, f, stream);
 }
 
 }  // namespace
@@ -91,13 +103,8 @@ int launch_mx8_expert_ffn(revive_ctx* ctx, const uint8_t* x, const uint8_t* x_sc
                           const void* const* w_gate_up, const void* const* w_down, void* y_perm, const void* w_sh_gate_up, const void* w_sh_down,
                           void* y_shared, int T, hipStream_t stream) {
   const Mx8Ffn f{x, x_scales, src_of, slot_offsets, w_gate_up, w_down, y_perm, w_sh_gate_up, w_sh_down, y_shared, T * ctx->cfg.k, y_shared ? T : 0};
-  // The tiles address a row of x by 32 bits.
-  if (f.N > kMx8TileRowsPerSlot * static_cast<int64_t>(ctx->P) && static_cast<int64_t>(T) * ctx->cfg.H < (1ll << 32)) {
-    const int rc = mx8_tile_product<EPI8_H>(ctx, f, stream);
-    return rc != REVIVE_OK ? rc : mx8_tile_product<EPI8_Y>(ctx, f, stream);
-  }
-  const int rc = mx8_stream_product<2, EPI8_H>(ctx, f, stream);
-  return rc != REVIVE_OK ? rc : mx8_stream_product<2, EPI8_Y>(ctx, f, stream);
+  const int rc = mx8_product<EPI8_H>(ctx, f, stream);
+  return rc != REVIVE_OK ? rc : mx8_product<EPI8_Y>(ctx, f, stream);
 }
 
 }  // namespace revive

@@ -8,6 +8,9 @@ namespace revive {
 
 namespace {
 
+// Workgroups of a form with tiles of `tile_m` rows and `width` columns.
+int64_t workgroups(const Mx8Problem& p, int tile_m, int width) { return static_cast<int64_t>(ceil_div(p.M, tile_m)) * ceil_div(p.n_out, width); }
+
 int too_large() { return fail(nullptr, REVIVE_EINVAL, "revive_mx_eight_linear: rows times N is more than one launch takes"); }
 
 template <int TMX, int W, int NW, int D>
@@ -24,6 +27,21 @@ int linear_tile(const Mx8Problem& base, hipStream_t stream) {
   a.dense = base;
   if (!mx8_cut(a.dense, ceil_div(base.M, kMx8Tile), 64 * TN, 512)) return too_large();
   return launch_mx8_tile<TN, EPI8_LINEAR>(nullptr, a, stream);
+}
+
+// The larger a workgroup's tile, the less is read per product, but a CU without a workgroup does nothing: the largest form that
+// gives nearly every CU one (the tiles through LDS, which multiply fastest, from three CUs of eight on).  us of 256 x 256 through
+// LDS, 64 x 64, 32 x 64, 16 x 64, 16 x 32, K = N = 7168: 16 rows - 19 18 18 13.9, 32 rows - 21 20 12.4 13.0, 64 rows - 24 13.9 20
+// 19, 128 rows 64 18 20 34 30, 256 rows 79 26 35 59 55, 512 rows 82 53 61, 1024 rows 89 93 117, 2048 rows 102 173 221; 4096 rows,
+// K = N = 2048 34 38 48; 1003 rows, K = 2048, N = 1411 36 12.9 14.2; 64 rows, K = 16384, N = 576 - 42 21 17 12.5.
+constexpr int kMx8FullGrid = 224, kMx8TileGrid = 96;
+
+int linear(const Mx8Problem& p, hipStream_t s) {
+  if (p.K >= 2 * kMx8Block && workgroups(p, kMx8Tile, 256) >= kMx8TileGrid) return linear_tile<4>(p, s);  // the tiles take K from two blocks on
+  if (workgroups(p, 64, 64) >= kMx8FullGrid) return linear_stream<4, 4, 4, 1>(p, s);
+  if (workgroups(p, 32, 64) >= kMx8FullGrid) return linear_stream<2, 4, 4, 2>(p, s);
+  if (workgroups(p, 16, 64) >= kMx8FullGrid) return linear_stream<1, 4, 8, 2>(p, s);
+  return linear_stream<1, 2, 8, 2>(p, s);
 }
 
 }  // namespace
@@ -55,9 +73,5 @@ extern "C" int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales,
   p.bias = bias; p.residual = static_cast<const uint16_t*>(residual); p.ld_residual = ld_residual;
   p.activation = activation;
   p.n_out = N; p.K = K; p.M = rows;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (rows <= 16) return linear_stream<1, 2, 8, 2>(p, s);
-  if (rows <= 128 || K < 64) return linear_stream<2, 4, 4, 2>(p, s);  // the tiles take K from two blocks on
-  if (static_cast<int64_t>(rows) * N < 256 * 256 * 128) return linear_stream<2, 4, 4, 2>(p, s);
-  return linear_tile<4>(p, s);
+  return linear(p, static_cast<hipStream_t>(stream));
 }

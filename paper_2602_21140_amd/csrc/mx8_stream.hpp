@@ -24,7 +24,8 @@ constexpr size_t mx8_stream_lds() {
   return loop > sums ? loop : sums;
 }
 
-template <int TMX, int W, int NW, int D, int EPI>
+// WIDE: rows of A that are reached by 64 bits (otherwise all of A, or of a dense problem's tile, is within 4 GiB).
+template <int TMX, int W, int NW, int D, int EPI, bool WIDE>
 __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(Mx8Args a) {
   static_assert(W % 2 == 0 && W <= 4 && (EPI != EPI8_H || W == 4) && NW > 1, "output columns in sets of 32, sums by way of LDS");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -40,14 +41,15 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
   // 16-row blocks of weights: where a lane's codes and scales of step 0 are
   constexpr int PER = W < 4 ? W : W / (EPI == EPI8_H ? 2 : 1);  // blocks side by side in a panel
   const int block0 = t.n_idx * PER, panel = block0 >> 3, sub0 = block0 & 7;
-  const uint8_t* codes[W];
-  const uint8_t* scales[EPI == EPI8_H ? 2 : 1];
+  constexpr int HALVES = EPI == EPI8_H ? 2 : 1;
+  uint64_t codes[HALVES], scales[HALVES];
 #pragma unroll
-  for (int s = 0; s < W; ++s)
-    codes[s] = t.B + (EPI == EPI8_H && s >= W / 2 ? g.b_half : 0) + static_cast<int64_t>(panel) * KT * kMx8PanelStep + (sub0 + s % PER) * 2048 + lane * 16;
-#pragma unroll
-  for (int h = 0; h < (EPI == EPI8_H ? 2 : 1); ++h)
-    scales[h] = t.B + (h ? g.b_half : 0) + g.b_codes + static_cast<int64_t>(panel) * KT * kMx8PanelScales + lane * 8 + sub0;
+  for (int h = 0; h < HALVES; ++h) {
+    const uint64_t matrix = reinterpret_cast<uint64_t>(t.B) + (h ? g.b_half : 0);
+    codes[h] = mx8_uniform(matrix + static_cast<int64_t>(panel) * KT * kMx8PanelStep + sub0 * 2048);
+    scales[h] = mx8_uniform(matrix + g.b_codes + static_cast<int64_t>(panel) * KT * kMx8PanelScales + sub0);
+  }
+  const uint32_t lane16 = lane * 16, lane8 = lane * 8;
   auto source = [&](int r) -> int64_t {  // row of A; rows past the tile read its last row again
     const int row = t.row_begin + min(r, rows - 1);
     return g.src_of ? g.src_of[row] / g.k : row;
@@ -57,18 +59,33 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
     constexpr int TM = decltype(tm_tag)::value;
     constexpr bool ONCE = decltype(once_tag)::value;  // streamed past the caches' retention (non-temporal)
     // load j of row-tile i: rows 16 i + 8 j + l / 8, chunk l % 8
-    const uint8_t* x[TM][2];
-    const uint8_t* xs[TM];  // rows 16 i + l / 4
+    typedef typename std::conditional<WIDE, int64_t, uint32_t>::type Off;
+    const int64_t origin = g.src_of ? 0 : t.row_begin;
+    const uint64_t A = mx8_uniform(reinterpret_cast<uint64_t>(g.A) + origin * g.a_row), A_scales = mx8_uniform(reinterpret_cast<uint64_t>(g.A_scales) + origin * blocks);
+    Off x[TM][2], xs[TM];  // scales: rows 16 i + l / 4
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) x[i][j] = g.A + source(i * 16 + j * 8 + (lane >> 3)) * g.a_row + (lane & 7) * 16;
-      xs[i] = g.A_scales + source(i * 16 + (lane >> 2)) * blocks;
+      for (int j = 0; j < 2; ++j) x[i][j] = static_cast<Off>((source(i * 16 + j * 8 + (lane >> 3)) - origin) * g.a_row + (lane & 7) * 16);
+      xs[i] = static_cast<Off>((source(i * 16 + (lane >> 2)) - origin) * blocks);
     }
     unsigned char* own = smem + wave * mx8_stream_wave_lds<TM>();
     uint32_t* own_scales = reinterpret_cast<uint32_t*>(own + 16 * TM * kMx8Step);
     // row r at r * 128 bytes, its chunk c at chunk c ^ ((r >> 1) & 7)
     auto place = [&](int row, int chunk) { return reinterpret_cast<mx8_u32x4*>(own + row * 128 + ((chunk ^ swz(row)) << 4)); };
+    // What the wavefront finishes: TM row-tiles of PAIRS sets of 32 columns are dealt round-robin.  A lane holds eight consecutive
+    // output columns 8 (l / 16) of activation row l % 16.  Bias and residual are asked for now.
+    constexpr int PAIRS = EPI == EPI8_H ? 1 : W / 2, ITEMS = (TM * PAIRS + NW - 1) / NW;
+    static_assert(NW % PAIRS == 0, "a wavefront's columns are the same in all of its row-tiles");
+    auto row_of = [&](int n) { return t.row_begin + (wave + n * NW) / PAIRS * 16 + r16; };
+    auto col_of = [&]() { return (block0 + 2 * (wave % PAIRS)) * 16 + kb * 8; };
+    uint32_t bias[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    mx8_u32x4 residual[ITEMS];
+    if (EPI == EPI8_LINEAR && wave < TM * PAIRS) {
+      if (g.bias) mx8_load8<float, false>(g.bias, col_of(), g.n_out, bias);
+#pragma unroll
+      for (int n = 0; n < ITEMS; ++n) residual[n] = mx8_residual8(g, min(row_of(n), t.row_end - 1), col_of());
+    }
     mx8_f32x4 acc[W][TM];
 #pragma unroll
     for (int s = 0; s < W; ++s)
@@ -76,26 +93,25 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
       for (int i = 0; i < TM; ++i) acc[s][i] = mx8_f32x4{0.f, 0.f, 0.f, 0.f};
 
     struct Step { Mx8Frag w[W]; uint32_t ws; mx8_u32x4 x[TM][2]; };
-    auto word = [](const uint8_t* p) { typedef uint32_t any __attribute__((aligned(1))); return *reinterpret_cast<const __attribute__((address_space(1))) any*>(reinterpret_cast<uintptr_t>(p)); };
+    typedef uint32_t any32 __attribute__((aligned(1)));
+#define REVIVE_GLOBAL(type, base, offset) reinterpret_cast<const __attribute__((address_space(1))) type*>((base) + (offset))
     auto load_w = [&](Step& b, int step) {
 #pragma unroll
       for (int s = 0; s < W; ++s) {
-        const auto p = reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(codes[s] + static_cast<int64_t>(step) * kMx8PanelStep));
+        const auto p = REVIVE_GLOBAL(mx8_u32x4, codes[HALVES * s / W] + static_cast<uint64_t>(step) * kMx8PanelStep + s % PER * 2048, lane16);
         b.w[s] = ONCE ? mx8_frag(__builtin_nontemporal_load(p), __builtin_nontemporal_load(p + 64)) : mx8_frag(p[0], p[64]);
       }
-      const int64_t at = static_cast<int64_t>(step) * kMx8PanelScales;
-      auto two = [&](const uint8_t* p) { return static_cast<uint32_t>(*reinterpret_cast<const __attribute__((address_space(1))) uint16_t*>(reinterpret_cast<uintptr_t>(p + at))); };
-      if (EPI == EPI8_H) b.ws = two(scales[0]) | two(scales[1]) << 16;
-      else if (W == 2) b.ws = two(scales[0]);
-      else b.ws = word(scales[0] + at);
+      const uint64_t at = static_cast<uint64_t>(step) * kMx8PanelScales;
+      if (EPI == EPI8_H) b.ws = *REVIVE_GLOBAL(uint16_t, scales[0] + at, lane8) | static_cast<uint32_t>(*REVIVE_GLOBAL(uint16_t, scales[HALVES - 1] + at, lane8)) << 16;
+      else if (W == 2) b.ws = *REVIVE_GLOBAL(uint16_t, scales[0] + at, lane8);
+      else b.ws = *REVIVE_GLOBAL(any32, scales[0] + at, lane8);
     };
     auto load = [&](Step& b, int step) {  // a whole step
       load_w(b, step);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          b.x[i][j] = *reinterpret_cast<const __attribute__((address_space(1))) mx8_u32x4*>(reinterpret_cast<uintptr_t>(x[i][j] + static_cast<int64_t>(step) * kMx8Step));
+        for (int j = 0; j < 2; ++j) b.x[i][j] = *REVIVE_GLOBAL(mx8_u32x4, A + static_cast<uint64_t>(step) * kMx8Step, x[i][j]);
     };
     auto multiply = [&](const Step& b, int at) {  // `at`: the step's place among the scales
 #pragma unroll
@@ -118,7 +134,7 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int p = 0; p < kMx8ScaleSteps / 4; ++p) scale[i][p] = word(xs[i] + min(first + 4 * p + (lane & 3), last - 1) * 4);
+        for (int p = 0; p < kMx8ScaleSteps / 4; ++p) scale[i][p] = *REVIVE_GLOBAL(any32, A_scales, xs[i] + static_cast<Off>(min(first + 4 * p + (lane & 3), last - 1) * 4));
       Step b[D];
 #pragma unroll
       for (int u = 0; u < D; ++u)
@@ -150,14 +166,16 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
       for (int i = 0; i < TM; ++i) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const mx8_u32x4 v = *reinterpret_cast<const mx8_u32x4*>(x[i][j] + (in ? static_cast<int64_t>(whole) * kMx8Step : -(lane & 7) * 16));
+          const mx8_u32x4 v = *REVIVE_GLOBAL(mx8_u32x4, A, in ? x[i][j] + static_cast<Off>(whole) * kMx8Step : x[i][j] - (lane & 7) * 16);
           b.x[i][j] = in ? v : mx8_u32x4{0u, 0u, 0u, 0u};
         }
         const int block = lane & 3;
-        reinterpret_cast<uint8_t*>(own_scales + (i * 16 + (lane >> 2)) * kMx8ScaleRow)[block] = block * 32 < left ? xs[i][whole * 4 + block] : 0;
+        reinterpret_cast<uint8_t*>(own_scales + (i * 16 + (lane >> 2)) * kMx8ScaleRow)[block] =
+            block * 32 < left ? *REVIVE_GLOBAL(uint8_t, A_scales, xs[i] + static_cast<Off>(whole * 4 + block)) : 0;
       }
       multiply(b, 0);
     }
+#undef REVIVE_GLOBAL
 
     // the wavefronts' sums, tile by tile; NW tiles at a time are added up, a wavefront each its own
     mx8_f32x4* part = reinterpret_cast<mx8_f32x4*>(smem);
@@ -172,11 +190,11 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
       for (int w = 1; w < NW; ++w) v += part[((w * W + s) * TM + i) * 64 + lane];
       return v;
     };
-    // a lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16
-    constexpr int PAIRS = EPI == EPI8_H ? 1 : W / 2;
-    for (int item = wave; item < TM * PAIRS; item += NW) {
-      const int i = item / PAIRS, p = item - i * PAIRS;
-      const int row = t.row_begin + i * 16 + r16, col = (block0 + 2 * p) * 16 + kb * 8;
+#pragma unroll
+    for (int n = 0; n < ITEMS; ++n) {
+      const int item = wave + n * NW, i = item / PAIRS, p = item % PAIRS;
+      if (item >= TM * PAIRS) break;
+      const int row = row_of(n), col = col_of();
       const mx8_f32x4 v0 = total(2 * p, i), v1 = total(2 * p + 1, i);
       if (EPI == EPI8_H) {
         uint32_t byte;
@@ -184,10 +202,18 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
         if (row >= t.row_end || col >= g.n_out) continue;
         *reinterpret_cast<uint2*>(g.H + static_cast<int64_t>(row) * g.n_out + col) = out;
         if (kb == 0) g.H_scales[static_cast<int64_t>(row) * (g.n_out >> 5) + (col >> 5)] = static_cast<uint8_t>(byte);
-      } else if (row < t.row_end) {
+      } else if (row < t.row_end && col < g.n_out) {
         float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-        if (EPI == EPI8_LINEAR) mx8_store_linear(g, row, col, v);
-        else if (col < g.n_out) mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(row) * g.n_out, col, g.n_out, v);
+        if (EPI == EPI8_LINEAR) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(bias[j]);
+          if (g.activation != REVIVE_ACT_NONE)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = mx8_activated(v[j], g.activation);
+          mx8_finish8(g, row, col, v, residual[n]);
+        } else {
+          mx8_store8<uint16_t, false>(g.Y + static_cast<int64_t>(row) * g.n_out, col, g.n_out, v);
+        }
       }
     }
   };
@@ -198,12 +224,12 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
   else run(std::integral_constant<int, TMX>{}, Y{});
 }
 
-template <int TMX, int W, int NW, int D, int EPI>
+template <int TMX, int W, int NW, int D, int EPI, bool WIDE = false>
 int launch_mx8_stream(const revive_ctx* ctx, const Mx8Args& args, hipStream_t stream) {
   const int grid = args.dense.blocks + args.grouped.blocks;
   if (grid <= 0) return REVIVE_OK;
   constexpr size_t lds = mx8_stream_lds<TMX, W, NW>();
-  auto kern = mx8_stream_kernel<TMX, W, NW, D, EPI>;
+  auto kern = mx8_stream_kernel<TMX, W, NW, D, EPI, WIDE>;
   if (lds > 64 * 1024) REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
   hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * NW), lds, stream, args);
   return check_hip(ctx, hipGetLastError(), "mx8_stream launch");

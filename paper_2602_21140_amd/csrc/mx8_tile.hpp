@@ -19,6 +19,11 @@
 
 namespace revive {
 
+// As copy_to_lds_16B, past the caches' retention: for weights that one workgroup, or a few at the same time, read.
+__device__ __forceinline__ void mx8_copy_once(uint32_t dst, uint64_t src, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(off), "s"(src), "s"(dst) : "memory", "m0");
+}
+
 constexpr int kMx8Tile = 256;  // rows of a workgroup
 template <int TN>
 struct Mx8TileShape {
@@ -60,11 +65,6 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
     const int row = min(r, rows - 1);
     return g.src_of ? g.src_of[t.row_begin + row] / g.k : row;
   };
-  auto uniform64 = [](uint64_t v) {
-    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32)));
-    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(v)));
-    return (static_cast<uint64_t>(hi) << 32) | lo;
-  };
   const int64_t first = g.src_of ? 0 : t.row_begin;  // the row that `source` counts from
   const int left = g.K & (kMx8Step - 1);             // K-elements of a last step that is not whole
   // copy i of A: rows 128 (i / 2) + 16 wave + 8 (i % 2) + l / 8
@@ -79,16 +79,16 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   };
   constexpr int WAVES_A_PANEL = 8 / S::PANELS;
   const int own_panel = wave / WAVES_A_PANEL;
-  uint64_t base_a = uniform64(reinterpret_cast<uint64_t>(g.A) + first * g.a_row);
-  uint64_t base_b = uniform64(reinterpret_cast<uint64_t>(t.B) + (EPI == EPI8_H && own_panel ? g.b_half : 0) +
+  uint64_t base_a = mx8_uniform(reinterpret_cast<uint64_t>(g.A) + first * g.a_row);
+  uint64_t base_b = mx8_uniform(reinterpret_cast<uint64_t>(t.B) + (EPI == EPI8_H && own_panel ? g.b_half : 0) +
                               static_cast<int64_t>(matrix(own_panel)) * KT * kMx8PanelStep + (wave % WAVES_A_PANEL) * (CP_B * 1024));
   // of the scales, lanes 0 to 31 take the first panel's, the others the second's; a wavefront 8 / PANELS of each
   constexpr int WS_LANES = 4 * S::PANELS;
   const int ws_lane = wave * WS_LANES + (lane & (WS_LANES - 1));
   const uint32_t ws_off = static_cast<uint32_t>(ws_lane >= 32 ? (EPI == EPI8_H ? g.b_half : static_cast<int64_t>(matrix(1) - matrix(0)) * KT * kMx8PanelScales) : 0) + (ws_lane & 31) * 16;
-  uint64_t base_ws = uniform64(reinterpret_cast<uint64_t>(t.B) + g.b_codes + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
+  uint64_t base_ws = mx8_uniform(reinterpret_cast<uint64_t>(t.B) + g.b_codes + static_cast<int64_t>(matrix(0)) * KT * kMx8PanelScales);
   const uint32_t xs_off = static_cast<uint32_t>(source(wave * 32 + (lane & 31)) * k_blocks);
-  uint64_t base_xs = uniform64(reinterpret_cast<uint64_t>(g.A_scales) + first * k_blocks);
+  uint64_t base_xs = mx8_uniform(reinterpret_cast<uint64_t>(g.A_scales) + first * k_blocks);
   // Five wait states before a copy may read a scalar register that a vector instruction wrote.
   asm volatile("s_nop 4" : "+s"(base_a), "+s"(base_b), "+s"(base_ws), "+s"(base_xs));
   const uint32_t lane16 = lane * 16;
@@ -102,7 +102,10 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
     copy_to_lds_16B(to(stage * S::STAGE_A + a_row(i) * 128), base_a + static_cast<uint64_t>(kt) * kMx8Step, off);
   };
   auto copy_b = [&](int kt, int stage, int i) {
-    copy_to_lds_16B(to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024), base_b + static_cast<uint64_t>(kt) * kMx8PanelStep + i * 1024, lane16);
+    const uint32_t dst = to(S::B + stage * S::STAGE_B + (wave * CP_B + i) * 1024);
+    const uint64_t src = base_b + static_cast<uint64_t>(kt) * kMx8PanelStep + i * 1024;
+    if (EPI == EPI8_LINEAR) copy_to_lds_16B(dst, src, lane16);
+    else mx8_copy_once(dst, src, lane16);  // 279 slots of 228 rows 3690 -> 3610 us, 108 slots of 450 2560 -> 2510, 12 of 1400 the same
   };
   auto copy_ws = [&](int kt, int stage) {
     if (lane < WS_LANES) copy_to_lds_16B(to(S::WS + stage * S::STAGE_WS + wave * (WS_LANES * 16)), base_ws + static_cast<uint64_t>(kt) * kMx8PanelScales, ws_off);
@@ -333,7 +336,7 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
 #pragma unroll
           for (int i = 0; i < TURNS; ++i) {
             const int row = min((tm * 2 + wm) * 16 + i * (64 / LANES) + r0, rows - 1);
-            res[tm][i] = whole ? mx8_load_any<false>(g.residual + (t.row_begin + row) * g.ld_residual + col) : mx8_u32x4{0u, 0u, 0u, 0u};
+            res[tm][i] = mx8_residual8(g, t.row_begin + row, col);
           }
       }
       uint32_t bias[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
@@ -364,18 +367,7 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
           if (row >= rows) continue;
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(bias[j]);
-          if (g.residual) {
-            uint32_t bits[8];
-            if (whole) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) bits[j] = (j & 1) ? res[tm][i][j / 2] & 0xFFFF0000u : res[tm][i][j / 2] << 16;
-            } else {
-              mx8_load8<uint16_t, false>(g.residual + (t.row_begin + row) * g.ld_residual, col, g.n_out, bits);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += __uint_as_float(bits[j]);
-          }
-          mx8_store8<uint16_t, false>(g.Y + (t.row_begin + row) * g.ldy, col, g.n_out, v);
+          if (col < g.n_out) mx8_finish8(g, t.row_begin + row, col, v, res[tm][i]);
         }
       }
     } else {
