@@ -352,20 +352,21 @@ def mx_pack_expert(gate: torch.Tensor, up: torch.Tensor, down: torch.Tensor) -> 
 ACTIVATION = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 
-def _here(stream, *tensors):
-    """All of them (None aside) are in the memory of the current device, on which a call without a context launches."""
-    device = None
+def _stream_of(stream, *tensors) -> int:
+    """The stream's handle, once all of the tensors (None aside) are found to be in the memory of the current device, on which a call
+    without a context launches."""
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
+        if t is not None and not t.is_cuda:
             raise ValueError(f"{tuple(t.shape)} {t.dtype}: in device memory expected")
-        if device is None:
-            device = torch.cuda.current_device()
-        if t.get_device() != device:
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
             raise ValueError(f"{tuple(t.shape)} {t.dtype} is on {t.device}, the current device is {device}")
-    if stream is not None and device is not None and stream.device_index != device:
-        raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")
+    if stream is not None:
+        if stream.device_index != device:
+            raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")
+        return stream.cuda_stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
 
 
 def _mx8_check_form(codes: torch.Tensor, scales: torch.Tensor, rows: int, n: int):
@@ -387,8 +388,8 @@ def mx8_quantize(x: torch.Tensor, out=None, stream=None) -> Tuple[torch.Tensor, 
     n = (K + MX_BLOCK - 1) // MX_BLOCK
     codes, scales = _mx8_form(rows, n, x.device) if out is None else out
     _mx8_check_form(codes, scales, rows, n)
-    _here(stream, x, codes, scales)
-    _check_free(lib().revive_mx_eight_quantize(x.data_ptr(), dtype, rows, K, ld, codes.data_ptr(), scales.data_ptr(), _current_stream(stream)))
+    s = _stream_of(stream, x, codes, scales)
+    _check_free(lib().revive_mx_eight_quantize(x.data_ptr(), dtype, rows, K, ld, codes.data_ptr(), scales.data_ptr(), s))
     return codes, scales
 
 
@@ -402,8 +403,8 @@ def mx8_dequantize(codes: torch.Tensor, scales: torch.Tensor, K: Optional[int] =
     if K is not None and width != K:
         raise ValueError(f"out {tuple(out.shape)}: {K} columns expected")
     _mx8_check_form(codes, scales, rows, (width + MX_BLOCK - 1) // MX_BLOCK)
-    _here(stream, codes, scales, out)
-    _check_free(lib().revive_mx_eight_dequantize(codes.data_ptr(), scales.data_ptr(), rows, width, code, out.data_ptr(), ld, _current_stream(stream)))
+    s = _stream_of(stream, codes, scales, out)
+    _check_free(lib().revive_mx_eight_dequantize(codes.data_ptr(), scales.data_ptr(), rows, width, code, out.data_ptr(), ld, s))
     return out
 
 
@@ -424,8 +425,8 @@ def mx8_pack(codes: torch.Tensor, scales: torch.Tensor, out=None, stream=None) -
         out = torch.empty(n, dtype=torch.uint8, device=codes.device)
     if out.dtype != torch.uint8 or out.numel() != n or not out.is_contiguous():
         raise ValueError(f"out: {n} contiguous bytes expected")
-    _here(stream, codes, scales, out)
-    _check_free(lib().revive_mx_eight_pack(codes.data_ptr(), scales.data_ptr(), rows, K, out.data_ptr(), _current_stream(stream)))
+    s = _stream_of(stream, codes, scales, out)
+    _check_free(lib().revive_mx_eight_pack(codes.data_ptr(), scales.data_ptr(), rows, K, out.data_ptr(), s))
     return out
 
 
@@ -452,7 +453,8 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     if residual is not None:
         if residual.dtype is not x.dtype or residual.shape != x.shape:
             raise ValueError(f"residual {residual.dtype} {tuple(residual.shape)}: {x.dtype} {tuple(x.shape)} expected")
-        ld_r = _mx_rows(residual, "residual")[3]
+        if not residual.is_contiguous():
+            ld_r = _mx_rows(residual, "residual")[3]
     _dense(weight, "weight", (H,), x.dtype)
     n = (H + MX_BLOCK - 1) // MX_BLOCK
     if out is None:
@@ -465,9 +467,9 @@ def add_rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
         raise ValueError("codes and scales are given exactly where quantize is true")
     if quantize:
         _mx8_check_form(codes, scales, rows, n)
-    _here(stream, x, weight, residual, total, y, codes, scales)
+    s = _stream_of(stream, x, weight, residual, total, y, codes, scales)
     _check_free(lib().revive_add_rms_norm(x.data_ptr(), _ptr(residual), weight.data_ptr(), dtype, rows, H, ld, ld_r, eps, _ptr(total), _ptr(y),
-                                          _ptr(codes), _ptr(scales), _current_stream(stream)))
+                                          _ptr(codes), _ptr(scales), s))
     return out
 
 
@@ -494,10 +496,11 @@ def mx8_linear(codes: torch.Tensor, scales: torch.Tensor, w: torch.Tensor, n_out
     if residual is not None:
         if residual.dtype is not out.dtype or residual.shape != out.shape:
             raise ValueError(f"residual {residual.dtype} {tuple(residual.shape)}: {out.dtype} {tuple(out.shape)} expected")
-        ld_r = _mx_rows(residual, "residual")[3]
-    _here(stream, codes, scales, w, bias, residual, out)
+        if not residual.is_contiguous():
+            ld_r = _mx_rows(residual, "residual")[3]
+    s = _stream_of(stream, codes, scales, w, bias, residual, out)
     _check_free(lib().revive_mx_eight_linear(codes.data_ptr(), scales.data_ptr(), rows, K, w.data_ptr(), n_out, _ptr(bias), ACTIVATION[activation],
-                                        _ptr(residual), ld_r, out.data_ptr(), ld, _current_stream(stream)))
+                                        _ptr(residual), ld_r, out.data_ptr(), ld, s))
     return out
 
 
@@ -792,11 +795,12 @@ class ReviveLayer:
             if y_shared is None or y_shared.dtype is not torch.bfloat16 or y_shared.numel() < T * H or not y_shared.is_contiguous() or not y_shared.is_cuda:
                 raise ValueError(f"y_shared: contiguous bfloat16 {(T, H)} in device memory expected, the shared expert's weights are given")
             shared = y_shared.data_ptr()
-        _here(stream, codes, scales, src_of, slot_offsets, w_sh_gate_up, w_sh_down, y_perm)
+        s = _stream_of(stream, codes, scales, src_of, slot_offsets, w_sh_gate_up, w_sh_down, y_perm, y_shared if shared is not None else None)
+        if codes.get_device() != (self.device.index or 0):
+            raise ValueError(f"the tensors are on {codes.device}, the layer is on {self.device}")
         tabs = self._mx8_tabs
         self._check(self.L.revive_mx_eight_expert_ffn(self._ctx, codes.data_ptr(), scales.data_ptr(), src_of.data_ptr(), slot_offsets.data_ptr(),
-                                                 tabs[0].data_ptr(), tabs[1].data_ptr(), y_perm.data_ptr(), gate_up, down, shared, T,
-                                                 _current_stream(stream)))
+                                                 tabs[0].data_ptr(), tabs[1].data_ptr(), y_perm.data_ptr(), gate_up, down, shared, T, s))
         return y_perm, y_shared
 
     def shared_ffn(self, x, w_sh_gate_up, w_sh_down, T: int, out=None, stream=None):

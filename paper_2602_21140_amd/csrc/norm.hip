@@ -21,132 +21,272 @@ struct NormArgs {
   uint8_t* codes; uint8_t* scales;  // [rows, 32 blocks], [rows, blocks]
 };
 
+// Sum over the wavefront, the same in every lane: four exchanges inside the rows of 16 lanes by cross-lane operands (through LDS,
+// as a shuffle goes, each takes ten times as long), then the rows' sums by scalar registers.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp(static_cast<int>(b), CTRL, 0xF, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp(static_cast<int>(b >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(b), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum(double v) {
+  v += dpp<0xB1>(v);   // lane ^ 1
+  v += dpp<0x4E>(v);   // lane ^ 2
+  v += dpp<0x141>(v);  // the half row mirrored
+  v += dpp<0x140>(v);  // the row mirrored
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+
+// Sum over the TPR threads of a row; `part`: a place of the workgroup's that nobody reads any more.
+template <int TPR>
+__device__ __forceinline__ double row_sum(double v, double* part) {
+  constexpr int WAVES = TPR / 64;
+  v = wave_sum(v);
+  if (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
 #pragma unroll
-  for (int i = 1; i < 64; i <<= 1) v += __shfl_xor(v, i);
+    for (int w = 0; w < WAVES; ++w) v += part[w];
+  }
   return v;
 }
 
-// TPR threads share a row, each with U units of eight numbers at a time, TPR units apart.  HELD: that is the whole row, which
-// stays in registers; otherwise the row is read twice.
-//
-// The squares are summed in fp64: no row is too large or too small for it, and the result does not hang on the order of the
-// sum, so that y's last bit, and with it the 8-bit form of a number next to a border, is the same for every shape of the kernel.
-template <typename El, int TPR, int U, bool HELD>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(NormArgs a) {
-  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1, WAVES = TPR / 64;
-  __shared__ double part[WAVES];
-  const int t = threadIdx.x & (TPR - 1);
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
-  if (row >= a.rows) return;  // with WAVES > 1, the whole workgroup
-  const El* x = static_cast<const El*>(a.x) + row * a.ld_x;
-  const El* residual = a.residual ? static_cast<const El*>(a.residual) + row * a.ld_residual : nullptr;
-  const El* weight = static_cast<const El*>(a.weight);
-  El* sum = a.sum ? static_cast<El*>(a.sum) + row * a.H : nullptr;
-  El* y = a.y ? static_cast<El*>(a.y) + row * a.H : nullptr;
-  const int blocks = (a.H + 31) >> 5;
+// 1 / sqrt(v) to fp64's last bits, from the instruction's some 26 bits by two Newton steps.
+__device__ __forceinline__ double inverse_root(double v) {
+  double r = __builtin_amdgcn_rsq(v);
+  if (!(v > 0. && v < __builtin_huge_val())) return r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) r = fma(0.5 * r, fma(-v * r, r, 1.), r);
+  return r;
+}
 
-  float v[U][8];
-  auto rounded = [](float f) { return sizeof(El) == 4 ? f : __uint_as_float(mx8_pack_bf16(f, f) << 16); };
-  auto load = [&](int c, bool first) {  // s of the units from c on
-    uint32_t bx[U][8], br[U][8];
+// Eight numbers as they are in memory.
+template <typename El>
+struct Raw { mx8_u32x4 w[sizeof(El) / 2]; };
+template <typename El, bool ONCE>
+__device__ __forceinline__ Raw<El> load_raw(const El* p) {
+  Raw<El> r;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int64_t k = static_cast<int64_t>(c + i * TPR + t) * 8;
-      mx8_load8<El, false>(x, k, a.H, bx[i]);
-      if (residual) mx8_load8<El, false>(residual, k, a.H, br[i]);
-    }
+  for (int i = 0; i < static_cast<int>(sizeof(El)) / 2; ++i) r.w[i] = mx8_load_any<ONCE>(p + i * (16 / sizeof(El)));
+  return r;
+}
+// Units u0, u0 + step, ... of a row of n numbers, zeros past it.  TAIL: n is no multiple of eight; the unit that the row ends in, one
+// lane's, is taken number by number.
+template <typename El, int U, bool ONCE, bool TAIL>
+__device__ __forceinline__ void load_units(Raw<El>* r, const El* row, int u0, int step, int n) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
+  for (int i = 0; i < U; ++i) {
+    if ((u0 + i * step) * 8 + 8 <= n) r[i] = load_raw<El, ONCE>(row + (u0 + i * step) * 8);
+    else
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[i][j] = __uint_as_float(bx[i][j]);
-        if (residual) v[i][j] = rounded(v[i][j] + __uint_as_float(br[i][j]));
-      }
-      if (first && sum) mx8_store8<El, false>(sum, static_cast<int64_t>(c + i * TPR + t) * 8, a.H, v[i]);
-    }
-  };
-  const int units = blocks * 4;
-  double square = 0;
-  for (int c = 0; c < units; c += U * TPR) {
-    load(c, true);
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) square = fma(static_cast<double>(v[i][j]), static_cast<double>(v[i][j]), square);
+      for (int j = 0; j < static_cast<int>(sizeof(El)) / 2; ++j) r[i].w[j] = mx8_u32x4{0u, 0u, 0u, 0u};
   }
-  square = wave_sum(square);
-  if (WAVES > 1) {
-    if ((t & 63) == 0) part[t >> 6] = square;
-    __syncthreads();
-    square = 0;
+  if (!TAIL) return;
+  const int last = n >> 3, i_last = (last - u0) / step;
+  if (last < u0 || (last - u0) % step != 0 || i_last >= U) return;
+  uint32_t b[8];
+  mx8_load8<El, false>(row, last * 8, n, b);
+  Raw<El> part;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) square += part[w];
-  }
-  const double inverse = 1.0 / sqrt(square / a.H + a.eps);
+  for (int i = 0; i < static_cast<int>(sizeof(El)) / 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part.w[i][j] = sizeof(El) == 4 ? b[4 * i + j] : b[2 * j] >> 16 | (b[2 * j + 1] & 0xFFFF0000u);
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (i == i_last) r[i] = part;
+}
+// The way back, of rounded numbers.
+template <typename El, int U, bool ONCE, bool TAIL>
+__device__ __forceinline__ void store_units(const float (*v)[8], El* row, int u0, int step, int n) {
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if ((u0 + i * step) * 8 + 8 <= n) mx8_store8<El, ONCE>(row, (u0 + i * step) * 8, 1 << 30, v[i]);
+  if (!TAIL) return;
+  const int last = n >> 3, i_last = (last - u0) / step;
+  if (last < u0 || (last - u0) % step != 0 || i_last >= U) return;
+  float part[8];
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i == i_last) part[j] = v[i][j];
+  mx8_store8<El, false>(row, last * 8, n, part);
+}
+template <typename El>
+__device__ __forceinline__ float number(const Raw<El>& r, int j) {
+  if (sizeof(El) == 4) return __uint_as_float(r.w[(j >> 2) & (sizeof(El) / 2 - 1)][j & 3]);
+  return __uint_as_float((j & 1) ? r.w[0][j >> 1] & 0xFFFF0000u : r.w[0][j >> 1] << 16);
+}
+template <typename El>
+__device__ __forceinline__ float rounded(float f) { return sizeof(El) == 4 ? f : __uint_as_float(mx8_pack_bf16(f, f) << 16); }
+
+// s -> y and its 8-bit form, of U units; four neighbouring lanes have a block's.
+template <typename El, int U, bool ONCE, bool TAIL>
+__device__ __forceinline__ void finish(const NormArgs& a, int64_t row, int u0, int step, float (*v)[8], const Raw<El>* weight, double inverse) {
+  const int blocks = (a.H + 31) >> 5;
   const float inv = static_cast<float>(inverse);
   const bool plain = inv > 0x1p-100f && inv < 0x1p+100f;  // else the product with s may be in fp32's range where inv is not
-  for (int c = 0; c < units; c += U * TPR) {
-    if (!HELD) {
-      if (sum) { x = sum; residual = nullptr; }  // where x or the residual was, if sum replaces it
-      load(c, false);
+  uint32_t byte[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float n = plain ? v[i][j] * inv : static_cast<float>(static_cast<double>(v[i][j]) * inverse);
+      v[i][j] = rounded<El>(n * number(weight[i], j));
+      if (TAIL && (u0 + i * step) * 8 + j >= a.H) v[i][j] = 0.f;  // not a NaN of zeros past the row
+      m = max(m, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
     }
-    uint32_t bw[U][8];
+    byte[i] = mx8_scale_byte(mx8_quad_max(m));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (a.y) store_units<El, U, ONCE, TAIL>(v, static_cast<El*>(a.y) + row * a.H, u0, step, a.H);
+  if (!a.codes) return;
 #pragma unroll
-    for (int i = 0; i < U; ++i) mx8_load8<El, false>(weight, static_cast<int64_t>(c + i * TPR + t) * 8, a.H, bw[i]);
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int u = c + i * TPR + t;
-      uint32_t m = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float n = plain ? v[i][j] * inv : static_cast<float>(static_cast<double>(v[i][j]) * inverse);
-        v[i][j] = static_cast<int64_t>(u) * 8 + j < a.H ? rounded(n * __uint_as_float(bw[i][j])) : 0.f;
-        m = max(m, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
-      }
-      const uint32_t byte = mx8_scale_byte(mx8_quad_max(m));
-      if (u >= units) continue;
-      if (y) mx8_store8<El, false>(y, static_cast<int64_t>(u) * 8, a.H, v[i]);
-      if (a.codes) {
-        *reinterpret_cast<uint2*>(a.codes + (row * blocks * 4 + u) * 8) = mx8_codes8(v[i], byte);
-        if ((u & 3) == 0) a.scales[row * blocks + (u >> 2)] = static_cast<uint8_t>(byte);
-      }
-    }
+  for (int i = 0; i < U; ++i) {
+    const int u = u0 + i * step;
+    if (u >= blocks * 4) continue;
+    *reinterpret_cast<uint2*>(a.codes + (row * blocks * 4 + u) * 8) = mx8_codes8(v[i], byte[i]);
+    if ((u & 3) == 0) a.scales[row * blocks + (u >> 2)] = static_cast<uint8_t>(byte[i]);
   }
 }
 
-// A grid has fewer than 2^32 threads in x (a launch of more runs what is left of them modulo 2^32, without an error).
-constexpr int64_t kMaxThreads = (1ll << 32) - 1024;
+// TPR threads share a row, each with U units of eight numbers, TPR units apart; a row's workgroup takes every gridDim-th row, with
+// the weights in registers and the next row on its way while one is finished.
+//
+// The squares are summed in fp64: no row is too large or too small for it, and the result does not hang on the order of the
+// sum, so that y's last bit, and with it the 8-bit form of a number next to a border, is the same for every shape of the kernel.
+// That costs nothing: what bounds it is HBM, and for few rows the chain of load, sum and store.
+// ONCE (more than the last-level cache holds): numbers past the caches' retention.
+template <typename El, int TPR, int U, bool ONCE, bool TAIL>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(NormArgs a) {
+  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+  __shared__ double part[2][TPR < 256 ? 1 : TPR / 64];
+  const int t = threadIdx.x & (TPR - 1);
+  const El* x = static_cast<const El*>(a.x);
+  const El* residual = static_cast<const El*>(a.residual);
+  Raw<El> rx[U], rr[U], rw[U];
+  auto load = [&](int64_t row) {
+    load_units<El, U, ONCE, TAIL>(rx, x + row * a.ld_x, t, TPR, a.H);
+    if (residual) load_units<El, U, ONCE, TAIL>(rr, residual + row * a.ld_residual, t, TPR, a.H);
+  };
+  int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+  const int64_t stride = static_cast<int64_t>(gridDim.x) * ROWS;
+  if (row >= a.rows) return;  // with more than one wavefront to a row, the whole workgroup
+  load(row);
+  load_units<El, U, false, TAIL>(rw, static_cast<const El*>(a.weight), t, TPR, a.H);
+  for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
+    float v[U][8];
+    double square = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[i][j] = number(rx[i], j);
+        if (residual) v[i][j] = rounded<El>(v[i][j] + number(rr[i], j));
+        square = fma(static_cast<double>(v[i][j]), static_cast<double>(v[i][j]), square);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // or all of the fp64 numbers are made first, and kept
+    }
+    if (a.sum) store_units<El, U, ONCE, TAIL>(v, static_cast<El*>(a.sum) + row * a.H, t, TPR, a.H);
+    if (row + stride < a.rows) load(row + stride);
+    const double inverse = inverse_root(row_sum<TPR>(square, part[turn]) / a.H + a.eps);
+    finish<El, U, ONCE, TAIL>(a, row, t, TPR, v, rw, inverse);
+  }
+}
 
-template <typename El, int TPR, int U, bool HELD>
-int launch(const NormArgs& base, hipStream_t stream) {
+// Rows that do not fit a workgroup's registers are read twice: by way of `sum` the second time, where there is one (x or the residual
+// may be what it replaces).
+template <typename El>
+__global__ __launch_bounds__(1024) void add_rms_norm_long_kernel(NormArgs a) {
+  constexpr int U = 2, TPR = 1024;
+  __shared__ double part[TPR / 64];
+  const int64_t row = blockIdx.x;
+  const int t = threadIdx.x, units = ((a.H + 31) >> 5) * 4;
+  const El* x = static_cast<const El*>(a.x) + row * a.ld_x;
+  const El* residual = a.residual ? static_cast<const El*>(a.residual) + row * a.ld_residual : nullptr;
+  El* sum = a.sum ? static_cast<El*>(a.sum) + row * a.H : nullptr;
+  float v[U][8];
+  auto load = [&](int c) {
+    Raw<El> rx[U], rr[U];
+    load_units<El, U, false, true>(rx, x, c + t, TPR, a.H);
+    if (residual) load_units<El, U, false, true>(rr, residual, c + t, TPR, a.H);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = residual ? rounded<El>(number(rx[i], j) + number(rr[i], j)) : number(rx[i], j);
+  };
+  double square = 0;
+  for (int c = 0; c < units; c += U * TPR) {
+    load(c);
+    if (sum) store_units<El, U, false, true>(v, sum, c + t, TPR, a.H);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) square = fma(static_cast<double>(v[i][j]), static_cast<double>(v[i][j]), square);
+    }
+  }
+  const double inverse = inverse_root(row_sum<TPR>(square, part) / a.H + a.eps);
+  if (sum) { x = sum; residual = nullptr; }
+  for (int c = 0; c < units; c += U * TPR) {
+    load(c);
+    Raw<El> rw[U];
+    load_units<El, U, false, true>(rw, static_cast<const El*>(a.weight), c + t, TPR, a.H);
+    finish<El, U, false, true>(a, row, c + t, TPR, v, rw, inverse);
+  }
+}
+
+constexpr int64_t kOnceBytes = 256ll << 20;
+constexpr int kNormGrid = 2048;  // workgroups that are resident at a time, and more: eight to a CU
+
+template <typename El, int TPR, int U>
+int launch(const NormArgs& a, hipStream_t stream) {
   constexpr int NT = TPR < 256 ? 256 : TPR;
+  const dim3 grid(static_cast<uint32_t>(std::min<int64_t>((a.rows * TPR + NT - 1) / NT, kNormGrid)));
+  const bool once = a.rows * a.H * static_cast<int64_t>(sizeof(El)) > kOnceBytes;
+  if (a.H % 8 != 0) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, true>), grid, dim3(NT), 0, stream, a);
+  else if (once) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, true, false>), grid, dim3(NT), 0, stream, a);
+  else hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, false>), grid, dim3(NT), 0, stream, a);
+  return check_hip(nullptr, hipGetLastError(), "add_rms_norm launch");
+}
+
+template <typename El>
+int launch_long(const NormArgs& base, hipStream_t stream) {
   NormArgs a = base;
   const int blocks = ceil_div(a.H, 32);
-  for (int64_t row = 0; row < base.rows; row += a.rows) {
-    a.rows = std::min<int64_t>(base.rows - row, kMaxThreads / TPR);
+  for (int64_t row = 0; row < base.rows; row += a.rows) {  // a grid has fewer than 2^32 threads
+    a.rows = std::min<int64_t>(base.rows - row, 1 << 21);
     a.x = static_cast<const El*>(base.x) + row * a.ld_x;
     if (a.residual) a.residual = static_cast<const El*>(base.residual) + row * a.ld_residual;
     if (a.sum) a.sum = static_cast<El*>(base.sum) + row * a.H;
     if (a.y) a.y = static_cast<El*>(base.y) + row * a.H;
     if (a.codes) { a.codes = base.codes + row * blocks * 32; a.scales = base.scales + row * blocks; }
-    const uint32_t grid = static_cast<uint32_t>((a.rows * TPR + NT - 1) / NT);
-    hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, HELD>), dim3(grid), dim3(NT), 0, stream, a);
+    hipLaunchKernelGGL(add_rms_norm_long_kernel<El>, dim3(static_cast<uint32_t>(a.rows)), dim3(1024), 0, stream, a);
     const int rc = check_hip(nullptr, hipGetLastError(), "add_rms_norm launch");
     if (rc != REVIVE_OK) return rc;
   }
   return REVIVE_OK;
 }
 
+// A unit a thread as long as a workgroup can hold the row: us of 1024 threads with one unit and 256 with four, bf16 with residual
+// and 8-bit output, H = 7168: 64 rows 4.8 (256 threads, weights loaded after the sum: 8.1), 1003 rows 16.8 and 16.2, 4096 rows 62 and
+// 57, 32 768 rows 392 (5.4 TB/s) and 413.  (Rows of an odd length begin at any address: 16 384 x 2839 bf16 163, 2.4 TB/s.)
 template <typename El>
 int launch_norm(const NormArgs& a, hipStream_t s) {
   const int units = ceil_div(a.H, 32) * 4;
-  if (units <= 64) return launch<El, 64, 1, true>(a, s);
-  if (units <= 256) return launch<El, 256, 1, true>(a, s);
-  if (units <= 512) return launch<El, 256, 2, true>(a, s);
-  if (units <= 1024) return launch<El, 256, 4, true>(a, s);
-  if (units <= 2048) return launch<El, 1024, 2, true>(a, s);
-  return launch<El, 1024, 2, false>(a, s);
+  if (units <= 64) return launch<El, 64, 1>(a, s);
+  if (units <= 256) return launch<El, 256, 1>(a, s);
+  if (units <= 512) return launch<El, 512, 1>(a, s);
+  if (units <= 1024) return launch<El, 1024, 1>(a, s);
+  if (units <= 2048 && sizeof(El) == 2) return launch<El, 1024, sizeof(El) == 2 ? 2 : 1>(a, s);
+  return launch_long<El>(a, s);
 }
 
 }  // namespace
