@@ -455,7 +455,8 @@ int revive_add_rms_norm(const void* x, const void* residual /*nullable*/, const 
  * activations and weights:  out = act(x W^T + bias) + residual, fp32 sums (with what the
  * note below says), one rounding to bf16.
  *   x, x_scales  dev: codes [rows, K], 16-byte aligned, and scales [rows, K/32]; K a
- *                multiple of 32 (a row of another length comes filled up with zeros)
+ *                multiple of 32 (a row of another length comes filled up with zeros);
+ *                rows <= 2^30, and no more outputs than one launch has tiles for
  *   w            dev: packed [N, K] (revive_mx_eight_pack), N * K < 2^32
  *   bias         dev fp32 [N]; NULL: none
  *   activation   REVIVE_ACT_*: none, max(z, 0), z / (1 + exp(-z)), z times the normal

@@ -355,13 +355,12 @@ ACTIVATION = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 def _stream_of(stream, *tensors) -> int:
     """The stream's handle, once all of the tensors (None aside) are found to be in the memory of the current device, on which a call
     without a context launches."""
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is not None and not t.is_cuda:
-            raise ValueError(f"{tuple(t.shape)} {t.dtype}: in device memory expected")
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"{tuple(t.shape)} {t.dtype} is on {t.device}, the current device is {device}")
+        if t is not None and (t.get_device() != device or device < 0):
+            raise ValueError(f"{tuple(t.shape)} {t.dtype} is on {t.device}: all in the memory of the current device expected")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
     if stream is not None:
         if stream.device_index != device:
             raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")

@@ -133,8 +133,9 @@ def check_ffn(y, x, w, what):
     assert (off <= allowed).all(), (what, float((off / allowed).max()), np.argwhere(off > allowed)[:4].tolist())
     # All elements together, whose errors are independent: bf16's rounding is evenly spread, 2^-8 / sqrt(3) of them; of h, an error d
     # moves a number to the next code, s away, with the probability d / s, in the mean square d s: with d below 2^-12 of h's size and
-    # s 2^-3 of it, 2^-7.5 of y.
-    if y.size >= 1000:
+    # s 2^-3 of it, 2^-7.5 of y.  That is a mean over many: one number of four times h's size that moves is 4 * 2^-3 / sqrt(h.size) of y,
+    # 2^-8 where h has 2^14 numbers, of which 2^14 * 2^-9 = 32 move; of 400 numbers a single one is 2^-5.3.
+    if h.size >= 1 << 14:
         assert np.linalg.norm(off) <= 2.0 ** -7 * np.linalg.norm(want), what
 
 
