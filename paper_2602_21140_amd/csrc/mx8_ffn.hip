@@ -14,7 +14,17 @@ namespace revive {
 
 namespace {
 
+// Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below it
+// the streaming kernel: us of the two products, streaming (32 rows to a workgroup) and tiles, 288 slots, H = 7168, I = 2048: 14 rows
+// 2040 and 2230, 28 rows 2470 and 2400, 57 rows 3520 and 2630; 72 slots, H = 2048, I = 1408: 21 rows 130 and 133, 43 rows 213 and
+// 148, 84 rows 320 and 178.  The host knows no row counts: the average is over all slots, without rows or not.
+// Fewer tiles than kMx8TileGrid leave too many CUs without one; 64 rows to a workgroup of the streaming kernel then.
 constexpr int kMx8TileRowsPerSlot = 24, kMx8TileGrid = 96;
+// The tiles' sums of gate and up are those of the 8-bit instruction (mx8_product.hpp), after which some 6 of 10 000 numbers of h are
+// rounded to the neighbouring code: y's relative error is 0.0020 so, 0.0017 of it bf16's rounding, if there are many numbers to
+// even that out; of 400 000 numbers it was up to 0.0027.  Fewer than 2^20 numbers are left to the streaming kernel, whose sums
+// are exact, the shared expert's in a launch of their own if the routed ones are many.
+constexpr int64_t kMx8ManyNumbers = 1 << 20;
 
 struct Mx8Ffn {
   const uint8_t* x; const uint8_t* x_scales;
@@ -89,12 +99,20 @@ int mx8_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
   const revive_config& c = ctx->cfg;
   // All of x within 32 bits, as the tiles and the narrow form of the stream address it.
-  const bool wide = EPI == EPI8_H && static_cast<int64_t>(ctx->cfg.T_max) * c.H >= (1ll << 32);
+  const bool wide = EPI == EPI8_H && static_cast<int64_t>(c.T_max) * c.H >= (1ll << 32);
   if (wide) return mx8_stream_product<2, 4, 2, EPI, EPI == EPI8_H>(ctx, f, stream);
   if (f.N <= kMx8TileRowsPerSlot * static_cast<int64_t>(ctx->P)) return mx8_stream_product<2, 4, 2, EPI>(ctx, f, stream);
   const int columns = EPI == EPI8_H ? ceil_div(c.I, 128) : ceil_div(c.H, 256);
-  if (static_cast<int64_t>(std::max(ctx->P, f.N / kMx8Tile)) * columns >= kMx8TileGrid) return mx8_tile_product<EPI>(ctx, f, stream);
-  return mx8_stream_product<4, 4, 1, EPI>(ctx, f, stream);
+  const bool many = EPI != EPI8_H || static_cast<int64_t>(f.N) * c.I >= kMx8ManyNumbers;
+  if (!many || static_cast<int64_t>(std::max(ctx->P, f.N / kMx8Tile)) * columns < kMx8TileGrid) return mx8_stream_product<4, 4, 1, EPI>(ctx, f, stream);
+  if (EPI == EPI8_H && f.T > 0 && static_cast<int64_t>(f.T) * c.I_shared < kMx8ManyNumbers) {
+    Mx8Ffn routed = f, shared = f;
+    routed.T = 0;
+    shared.N = 0;
+    const int rc = mx8_tile_product<EPI>(ctx, routed, stream);
+    return rc != REVIVE_OK ? rc : mx8_stream_product<4, 4, 1, EPI>(ctx, shared, stream);
+  }
+  return mx8_tile_product<EPI>(ctx, f, stream);
 }
 
 }  // namespace

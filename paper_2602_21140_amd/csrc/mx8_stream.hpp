@@ -9,6 +9,11 @@
 // of the activations a load takes whole lines, 8 rows of 128 bytes, and the wavefront turns them to operand order in LDS of its
 // own (as operands straight from memory, 16 rows of 64 bytes, a product of 64 rows takes twice as long).  Their scales come for
 // 16 steps at once.
+//
+// EPI8_H multiplies in bf16, which holds both operands' numbers, scales included, and whose products are added up in fp32.  An
+// h that is off by the 3e-5 of the 8-bit instruction is rounded to the next code, 2^-4 away, some 6 times in 10 000: with few rows
+// a single one of them shows (y of 8 rows, I = 896: relative error 0.0030, of which bf16's rounding is 0.0017).  The stream has the
+// time: 64 tokens on 279 slots of 7168 x 2048 take the same 1.53 ms.
 #pragma once
 
 #include "mx8_product.hpp"
@@ -92,7 +97,7 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
 #pragma unroll
       for (int i = 0; i < TM; ++i) acc[s][i] = mx8_f32x4{0.f, 0.f, 0.f, 0.f};
 
-    struct Step { Mx8Frag w[W]; uint32_t ws; mx8_u32x4 x[TM][2]; };
+    struct Step { Mx8Frag w[W]; uint32_t ws[HALVES]; mx8_u32x4 x[TM][2]; };  // EPI8_H: ws of the two halves of K
     typedef uint32_t any32 __attribute__((aligned(1)));
 #define REVIVE_GLOBAL(type, base, offset) reinterpret_cast<const __attribute__((address_space(1))) type*>((base) + (offset))
     auto load_w = [&](Step& b, int step) {
@@ -102,9 +107,14 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
         b.w[s] = ONCE ? mx8_frag(__builtin_nontemporal_load(p), __builtin_nontemporal_load(p + 64)) : mx8_frag(p[0], p[64]);
       }
       const uint64_t at = static_cast<uint64_t>(step) * kMx8PanelScales;
-      if (EPI == EPI8_H) b.ws = *REVIVE_GLOBAL(uint16_t, scales[0] + at, lane8) | static_cast<uint32_t>(*REVIVE_GLOBAL(uint16_t, scales[HALVES - 1] + at, lane8)) << 16;
-      else if (W == 2) b.ws = *REVIVE_GLOBAL(uint16_t, scales[0] + at, lane8);
-      else b.ws = *REVIVE_GLOBAL(any32, scales[0] + at, lane8);
+      if (EPI == EPI8_H) {  // of the lane's own K-elements, 16 (l / 16) on: blocks l / 32 and 2 + l / 32
+        const uint32_t of_block = ((kb >> 1) * 16 + r16) * 8;
+#pragma unroll
+        for (int k = 0; k < HALVES; ++k)
+          b.ws[k] = *REVIVE_GLOBAL(uint16_t, scales[0] + at + k * 256, of_block) | static_cast<uint32_t>(*REVIVE_GLOBAL(uint16_t, scales[HALVES - 1] + at + k * 256, of_block)) << 16;
+      }
+      else if (W == 2) b.ws[0] = *REVIVE_GLOBAL(uint16_t, scales[0] + at, lane8);
+      else b.ws[0] = *REVIVE_GLOBAL(any32, scales[0] + at, lane8);
     };
     auto load = [&](Step& b, int step) {  // a whole step
       load_w(b, step);
@@ -118,11 +128,31 @@ __global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(M
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) *place(i * 16 + j * 8 + (lane >> 3), lane & 7) = b.x[i][j];
+      auto scale = [&](int i, int block) -> uint32_t { return reinterpret_cast<const uint8_t*>(own_scales + (i * 16 + r16) * kMx8ScaleRow + at)[block]; };
+      if constexpr (EPI == EPI8_H) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const Mx8Frag f = mx8_frag(*place(i * 16 + r16, kb), *place(i * 16 + r16, kb + 4));
-        const uint32_t scale = reinterpret_cast<const uint8_t*>(own_scales + (i * 16 + r16) * kMx8ScaleRow + at)[kb];
-        mx8_for_blocks<W>([&](auto s) { acc[s.value][i] = mx8_mfma<s.value, 0>(b.w[s.value], f, acc[s.value][i], b.ws, scale); });
+        for (int k = 0; k < 2; ++k) {
+          Mx8Wide f[TM];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) f[i] = mx8_widened(*place(i * 16 + r16, kb + 4 * k), scale(i, 2 * k + (kb >> 1)));
+#pragma unroll
+          for (int s = 0; s < W; ++s) {
+            const mx8_u32x4 codes = {static_cast<uint32_t>(b.w[s][4 * k]), static_cast<uint32_t>(b.w[s][4 * k + 1]), static_cast<uint32_t>(b.w[s][4 * k + 2]), static_cast<uint32_t>(b.w[s][4 * k + 3])};
+            const Mx8Wide w = mx8_widened(codes, (b.ws[k] >> (8 * s)) & 255u);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+              for (int n = 0; n < 2; ++n) acc[s][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[n], f[i].part[n], acc[s][i], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);  // or all blocks are widened first, and kept
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          const Mx8Frag f = mx8_frag(*place(i * 16 + r16, kb), *place(i * 16 + r16, kb + 4));
+          const uint32_t own = scale(i, kb);
+          mx8_for_blocks<W>([&](auto s) { acc[s.value][i] = mx8_mfma<s.value, 0>(b.w[s.value], f, acc[s.value][i], b.ws[0], own); });
+        }
       }
     };
 

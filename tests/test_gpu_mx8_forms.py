@@ -84,9 +84,9 @@ def test_tiles_in_a_graph():
 MANY = [1, 0, 16, 17, 64, 65, 100, 128, 129, 192, 193, 255, 256, 257, 300] + [5, 0, 40] * 12
 
 
-# tiles (more than 24 rows per slot on average and 96 tiles): K of whole and of broken steps, scales by words and by bytes, widths that end
-# inside a panel; the shared expert beside them
-@pytest.mark.parametrize("H,I,I_shared,k,T", [(512, 256, 0, 1, None), (576, 320, 192, 2, 1300), (1024, 512, 512, 1, 2700), (640, 192, 0, 3, None)])
+# tiles (more than 24 rows per slot on average, 96 tiles, 2^20 numbers of h): K of whole and of broken steps, scales by words and by bytes, widths that end
+# inside a panel; the shared expert beside them, in their launch and in its own
+@pytest.mark.parametrize("H,I,I_shared,k,T", [(512, 512, 0, 1, None), (576, 704, 192, 2, 1300), (1024, 512, 576, 1, 2700), (640, 704, 0, 3, None)])
 def test_ffn_by_tiles(H, I, I_shared, k, T):
     f = Ffn(H, I, k, MANY, I_shared, T, seed=H)
     f.check(*f.run())
@@ -102,7 +102,7 @@ def test_ffn_of_many_rows_in_few_slots(H, I, I_shared, k, rows, T):
 
 
 def test_ffn_by_tiles_of_rows_that_are_not_finite_and_in_a_graph():
-    f = Ffn(576, 320, 1, MANY, 192, sum(MANY), seed=3)
+    f = Ffn(576, 512, 1, MANY, 576, sum(MANY), seed=3)
     clean, clean_shared = (t.clone() for t in f.run())
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
