@@ -476,8 +476,10 @@ int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales, int32_t ro
 
 /* Expert FFN on microscaled 8-bit weights and activations, for bf16 layers.  With Q the
  * rounding above along a row, for every slot p with rows [slot_offsets[p],
- * slot_offsets[p+1]):  h = Q(silu(x G_p) * (x U_p)),  y = h D_p, sums as of the product
- * above, and the same on all T rows of x for the shared expert when y_shared != NULL.
+ * slot_offsets[p+1]):  h = Q(silu(x G_p) * (x U_p)),  y = h D_p, and the same on all T rows
+ * of x for the shared expert when y_shared != NULL.  Sums as of the product above; those
+ * behind h are exact fp32 where there are few rows or few numbers of h, so that a token's
+ * result goes by T too, by an h that is rounded to the code beside.
  *   x, x_scales  dev: the tokens' codes [T, H], 16-byte aligned, and scales [T, H/32], not
  *              permuted (revive_add_rms_norm, revive_mx_eight_quantize)
  *   src_of     dev int32 [N] (revive_dispatch_index): row r is token src_of[r] / k

@@ -15,11 +15,12 @@ namespace revive {
 namespace {
 
 // Above so many rows per slot on average the tiles win, which read a slot's weights once per 256 rows and multiply faster, below it
-// the streaming kernel: us of the two products, streaming (32 rows to a workgroup) and tiles, 288 slots, H = 7168, I = 2048: 14 rows
-// 2040 and 2230, 28 rows 2470 and 2400, 57 rows 3520 and 2630; 72 slots, H = 2048, I = 1408: 21 rows 130 and 133, 43 rows 213 and
-// 148, 84 rows 320 and 178.  The host knows no row counts: the average is over all slots, without rows or not.
-// Fewer tiles than kMx8TileGrid leave too many CUs without one; 64 rows to a workgroup of the streaming kernel then.
-constexpr int kMx8TileRowsPerSlot = 24, kMx8TileGrid = 96;
+// the streaming kernel (64 rows to a workgroup).  us of both products, gate and up streamed and by tiles, down (gate and up streamed
+// 32 rows at a time) streamed and by tiles: 288 slots, H = 7168, I = 2048: 7 rows 1881 1954, 1877 1950, 25 rows 2318 2343, 2366 2391, 39 rows
+// 2700 2430, 2710 2660; 72 slots, H = 2048, I = 1408: 18 rows 127 124, 126 136, 27 rows 147 131, 147 155, 43 rows 172 139, 166 167, 84 rows 285
+// 190, 275 254.  The host knows no row counts: the average is over all slots, without rows or not.  Fewer tiles than kMx8TileGrid
+// leave too many CUs without one.
+constexpr int kMx8TileRowsGateUp = 24, kMx8TileRowsDown = 36, kMx8TileGrid = 96;
 // The tiles' sums of gate and up are those of the 8-bit instruction (mx8_product.hpp), after which some 6 of 10 000 numbers of h are
 // rounded to the neighbouring code: y's relative error is 0.0020 so, 0.0017 of it bf16's rounding, if there are many numbers to
 // even that out; of 400 000 numbers it was up to 0.0027.  Fewer than 2^20 numbers are left to the streaming kernel, whose sums
@@ -79,11 +80,14 @@ bool mx8_args(const revive_ctx* ctx, const Mx8Ffn& f, int tile_m, int width, int
 
 int too_large(const revive_ctx* ctx) { return fail(ctx, REVIVE_EINVAL, "revive_mx_eight_expert_ffn: rows times columns are more than one launch takes"); }
 
-template <int TMX, int W, int D, int EPI, bool WIDE = false>
+// 64 rows a workgroup: with 32, 64 tokens on 72 slots of 2048 x 1408 take 108 instead of 104 us, 700 of them 320 instead of 250, and a
+// token on 288 slots of 7168 x 2048 75.7 instead of 77.4.  WIDE, 32: the wider addresses of 64 do not fit in the registers.
+template <int EPI, bool WIDE = false>
 int mx8_stream_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
+  constexpr int TMX = WIDE ? 2 : 4, D = WIDE ? 2 : 1;
   Mx8Args a;
-  if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 16 * W, 256, a)) return too_large(ctx);
-  return launch_mx8_stream<TMX, W, 4, D, EPI, WIDE>(ctx, a, stream);
+  if (!mx8_args<EPI>(ctx, f, 16 * TMX, EPI == EPI8_H ? 32 : 64, 256, a)) return too_large(ctx);
+  return launch_mx8_stream<TMX, 4, 4, D, EPI, WIDE>(ctx, a, stream);
 }
 
 template <int EPI>
@@ -99,18 +103,18 @@ int mx8_product(revive_ctx* ctx, const Mx8Ffn& f, hipStream_t stream) {
   KernelTimer timer(ctx, EPI == EPI8_H ? REVIVE_K_MX8_GATE_UP : REVIVE_K_MX8_DOWN, stream);
   const revive_config& c = ctx->cfg;
   // All of x within 32 bits, as the tiles and the narrow form of the stream address it.
-  const bool wide = EPI == EPI8_H && static_cast<int64_t>(c.T_max) * c.H >= (1ll << 32);
-  if (wide) return mx8_stream_product<2, 4, 2, EPI, EPI == EPI8_H>(ctx, f, stream);
-  if (f.N <= kMx8TileRowsPerSlot * static_cast<int64_t>(ctx->P)) return mx8_stream_product<2, 4, 2, EPI>(ctx, f, stream);
+  if (EPI == EPI8_H && static_cast<int64_t>(c.T_max) * c.H >= (1ll << 32)) return mx8_stream_product<EPI, EPI == EPI8_H>(ctx, f, stream);
   const int columns = EPI == EPI8_H ? ceil_div(c.I, 128) : ceil_div(c.H, 256);
-  const bool many = EPI != EPI8_H || static_cast<int64_t>(f.N) * c.I >= kMx8ManyNumbers;
-  if (!many || static_cast<int64_t>(std::max(ctx->P, f.N / kMx8Tile)) * columns < kMx8TileGrid) return mx8_stream_product<4, 4, 1, EPI>(ctx, f, stream);
+  const bool tiles = f.N > (EPI == EPI8_H ? kMx8TileRowsGateUp : kMx8TileRowsDown) * static_cast<int64_t>(ctx->P) &&
+                     static_cast<int64_t>(std::max(ctx->P, f.N / kMx8Tile)) * columns >= kMx8TileGrid &&
+                     (EPI != EPI8_H || static_cast<int64_t>(f.N) * c.I >= kMx8ManyNumbers);
+  if (!tiles) return mx8_stream_product<EPI>(ctx, f, stream);
   if (EPI == EPI8_H && f.T > 0 && static_cast<int64_t>(f.T) * c.I_shared < kMx8ManyNumbers) {
     Mx8Ffn routed = f, shared = f;
     routed.T = 0;
     shared.N = 0;
     const int rc = mx8_tile_product<EPI>(ctx, routed, stream);
-    return rc != REVIVE_OK ? rc : mx8_stream_product<4, 4, 1, EPI>(ctx, shared, stream);
+    return rc != REVIVE_OK ? rc : mx8_stream_product<EPI>(ctx, shared, stream);
   }
   return mx8_tile_product<EPI>(ctx, f, stream);
 }

@@ -29,15 +29,19 @@ int linear_tile(const Mx8Problem& base, hipStream_t stream) {
   return launch_mx8_tile<TN, EPI8_LINEAR>(nullptr, a, stream);
 }
 
-// The larger a workgroup's tile, the less is read per product, but a CU without a workgroup does nothing: the largest form that
-// gives nearly every CU one (the tiles through LDS, which multiply fastest, from three CUs of eight on).  us of 256 x 256 through
-// LDS, 64 x 64, 32 x 64, 16 x 64, 16 x 32, K = N = 7168: 16 rows - 19 18 18 13.9, 32 rows - 21 20 12.4 13.0, 64 rows - 24 13.9 20
-// 19, 128 rows 64 18 20 34 30, 256 rows 79 26 35 59 55, 512 rows 82 53 61, 1024 rows 89 93 117, 2048 rows 102 173 221; 4096 rows,
-// K = N = 2048 34 38 48; 1003 rows, K = 2048, N = 1411 36 12.9 14.2; 64 rows, K = 16384, N = 576 - 42 21 17 12.5.
-constexpr int kMx8FullGrid = 224, kMx8TileGrid = 96;
+// The larger a workgroup's tile, the less is read per product, but a CU without a workgroup does nothing.  us of 256 x 256 and 256 x 128
+// through LDS, 64 x 64, 32 x 64, 16 x 64, 16 x 32, K = N = 7168: 16 rows - - 19 18 18 13.9, 32 rows - - 21 20 12.4 13.0, 64 rows - - 24 13.9
+// 20 19, 128 rows 64 41 18 20 34 30, 256 rows 79 50 27 35 59 55, 512 rows 82 55 54 61, 768 rows 82 61 76 88, 1024 rows 87 68 92 118, 1536
+// rows 95 113 137, 2048 rows 102 127 173 221; K = N = 2048: 2048 rows 30 21.2 21.2 26, 4096 rows 33 26 38 47; 8192 rows, K = N = 1024 23 18 27 33;
+// 1003 rows, K = 2048, N = 1411 37 25 13 14; 64 rows, K = 16384, N = 576 - - 42 21 17 12.5.
+// So the tiles through LDS, which multiply fastest, where they give half of the CUs one, those of 128 columns as long as none gets
+// two; else the largest form that gives nearly every CU one.
+constexpr int kMx8Cus = 256, kMx8HalfGrid = 128, kMx8FullGrid = 224;
 
 int linear(const Mx8Problem& p, hipStream_t s) {
-  if (p.K >= 2 * kMx8Block && workgroups(p, kMx8Tile, 256) >= kMx8TileGrid) return linear_tile<4>(p, s);  // the tiles take K from two blocks on
+  const int64_t tiles = p.K >= 2 * kMx8Block ? workgroups(p, kMx8Tile, 128) : 0;  // they take K from two blocks on
+  if (tiles > kMx8Cus) return linear_tile<4>(p, s);
+  if (tiles >= kMx8HalfGrid) return linear_tile<2>(p, s);
   if (workgroups(p, 64, 64) >= kMx8FullGrid) return linear_stream<4, 4, 4, 1>(p, s);
   if (workgroups(p, 32, 64) >= kMx8FullGrid) return linear_stream<2, 4, 4, 2>(p, s);
   if (workgroups(p, 16, 64) >= kMx8FullGrid) return linear_stream<1, 4, 8, 2>(p, s);

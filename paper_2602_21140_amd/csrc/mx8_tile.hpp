@@ -8,7 +8,14 @@
 // each piece is filled again at once, a step and a half before it is needed: at barrier X, after the first pair, the weights and
 // the activations of the first two pairs (everybody has read them), at barrier Y, after the third, those of the other two.  Each
 // barrier also publishes what was ordered a step and a half before; what was ordered since stays on its way.  With one barrier a
-// step, everything ordered at once, the copies and the products took turns.
+// step, everything ordered at once, the copies and the products took turns (8192 x 7168 x 7168 488 us, with the second barrier 424, with
+// the copies ordered one by one between the products 398, with bias and residual asked for early 380).
+//
+// What bounds it: 8192 x 7168 x 7168 takes 376 us, 2.24 PFLOP/s; 896 tiles are 3.5 rounds of the 256 CUs, and a step of a whole round takes 1.6 us, of
+// which the matrix instructions alone, on a chip that they fill, take 1.4 (power: on a quarter of the CUs they take 1.1).
+// With fewer workgroups than CUs a step still takes 1.0 us (TN = 2: 0.7 to 0.9), as long as LDS is read: 192 KiB of operands (160) and
+// 64 KiB of copies (48) at 128 bytes a cycle.  A third stage, tiles of 128 x 128 with four stages and one barrier: the same within 10 %, but for
+// 190 to 256 such tiles (512 x 7168 x 7168: 45 instead of 54 us).
 //
 // LDS: weights lie in operand order, as in memory.  Activation row r is at r * 128 bytes, its 16-byte chunk c at chunk
 // c ^ ((r >> 1) & 7): a fragment read (16 rows, four chunks) meets no bank twice in any of its four passes.  A step's scales of

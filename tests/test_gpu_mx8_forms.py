@@ -14,18 +14,20 @@ from test_gpu_mx8_linear import Product
 pytestmark = pytest.mark.gpu
 
 
-# tiles of 256 x 256 (96 of them and more): K of less than a step, of one, two, three, with a rest of 32, 64 and 96 behind each; groups of
-# four steps that end with the row and inside of it; rows that leave one, two, three and four pairs of the last row-tile to multiply
+# tiles of 256 x 256 and of 256 x 128 (256 of these and fewer): K of less than a step, of one, two, three, with a rest of 32, 64 and 96 behind
+# each; groups of four steps that end with the row and inside of it; rows that leave one, two, three and four pairs of the last row-tile to multiply
 @pytest.mark.parametrize("K", [64, 96, 128, 160, 192, 256, 288, 384, 480, 512, 640, 768, 896, 1024, 1152])
-def test_tiles(K):
-    p = Product(2305 + (K // 32) % 5 * 50, K, 2433)
+@pytest.mark.parametrize("N", [3457, 2433])
+def test_tiles(K, N):
+    p = Product(2305 + (K // 32) % 5 * 50, K, N)
     how = dict(bias=K % 64 == 0, activation=("none", "silu", "gelu", "relu")[K // 32 % 4], residual=K % 128 == 0 or K % 96 == 0)
     p.check(p.run(**how), **how)
 
 
 @pytest.mark.parametrize("K", [544, 512])
-def test_tiles_of_strided_and_unaligned_rows_in_place_and_not_finite(K):
-    rows, N = 2349, 2434
+@pytest.mark.parametrize("N", [3458, 2434])
+def test_tiles_of_strided_and_unaligned_rows_in_place_and_not_finite(K, N):
+    rows = 2349
     p = Product(rows, K, N, seed=6)
     want = p.run()
     p.check(want)
@@ -63,8 +65,9 @@ def test_streams(rows, N, K):
     p.check(p.run(bias=False, residual=False), bias=False, residual=False)
 
 
-def test_tiles_in_a_graph():
-    p = Product(2400, 640, 2432, seed=8)
+@pytest.mark.parametrize("N", [3456, 2432])
+def test_tiles_in_a_graph(N):
+    p = Product(2400, 640, N, seed=8)
     out = p.run()
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
@@ -84,7 +87,7 @@ def test_tiles_in_a_graph():
 MANY = [1, 0, 16, 17, 64, 65, 100, 128, 129, 192, 193, 255, 256, 257, 300] + [5, 0, 40] * 12
 
 
-# tiles (more than 24 rows per slot on average, 96 tiles, 2^20 numbers of h): K of whole and of broken steps, scales by words and by bytes, widths that end
+# tiles (more than 24 rows per slot on average, 36 for the second product, 96 tiles, 2^20 numbers of h): K of whole and of broken steps, scales by words and by bytes, widths that end
 # inside a panel; the shared expert beside them, in their launch and in its own
 @pytest.mark.parametrize("H,I,I_shared,k,T", [(512, 512, 0, 1, None), (576, 704, 192, 2, 1300), (1024, 512, 576, 1, 2700), (640, 704, 0, 3, None)])
 def test_ffn_by_tiles(H, I, I_shared, k, T):
@@ -93,7 +96,7 @@ def test_ffn_by_tiles(H, I, I_shared, k, T):
     f.L.close()
 
 
-# many rows to a slot and too few tiles for the chip: 64 rows to a workgroup
+# many rows to a slot and too few tiles for the chip
 @pytest.mark.parametrize("H,I,I_shared,k,rows,T", [(320, 192, 64, 1, [300, 0, 40], 340), (1152, 128, 0, 2, [64, 65, 63, 0, 1], None)])
 def test_ffn_of_many_rows_in_few_slots(H, I, I_shared, k, rows, T):
     f = Ffn(H, I, k, rows, I_shared, T, seed=I)
