@@ -419,8 +419,8 @@ int revive_mx_eight_dequantize(const uint8_t* codes, const uint8_t* scales, int6
                           void* out, int64_t ld, revive_stream stream);
 
 /* Weights of the 8-bit products: codes and scales of an output-major matrix [rows, K]
- * (K a multiple of 32, rows * K < 2^32) into the order in which the kernels read them.
- * revive_mx_eight_packed_bytes gives the size of `packed` (dev, 16-byte aligned).  Rows
+ * (K a multiple of 32 up to 2^24, rows * K < 2^32) into the order in which the kernels read
+ * them.  revive_mx_eight_packed_bytes gives the size of `packed` (dev, 16-byte aligned).  Rows
  * are filled up with zeros to a multiple of 128, K to one of 128.  Packed, a matrix is
  *   codes  [rows/128][K/128][8][2][64][16 bytes]: blocks of 16 rows x 128 K; lane
  *          l = 0..63 of a block's half h has K 64*h + 16*(l/16) .. +15 of its row l%16
@@ -455,7 +455,7 @@ int revive_add_rms_norm(const void* x, const void* residual /*nullable*/, const 
  * activations and weights:  out = act(x W^T + bias) + residual, fp32 sums (with what the
  * note below says), one rounding to bf16.
  *   x, x_scales  dev: codes [rows, K], 16-byte aligned, and scales [rows, K/32]; K a
- *                multiple of 32 (a row of another length comes filled up with zeros);
+ *                multiple of 32 up to 2^24 (a row of another length comes filled up with zeros);
  *                rows <= 2^30, and no more outputs than one launch has tiles for
  *   w            dev: packed [N, K] (revive_mx_eight_pack), N * K < 2^32
  *   bias         dev fp32 [N]; NULL: none

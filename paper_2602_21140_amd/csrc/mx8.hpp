@@ -22,6 +22,8 @@ constexpr int kMx8Panel = 128;                          // weight rows that are 
 constexpr int kMx8PanelStep = kMx8Panel * kMx8Step;     // bytes of a panel's codes for one step
 constexpr int kMx8PanelScales = kMx8Panel * kMx8Step / kMx8Block;
 
+constexpr int kMx8MaxK = 1 << 24;                       // of a product: the kernels reach 256 rows of codes by 32 bits
+
 __host__ __device__ inline int mx8_steps(int K) { return (K + kMx8Step - 1) / kMx8Step; }
 
 // Packed weights: [panels][steps][8][2][64][16] bytes of codes, then [panels][steps][64][8] bytes of scales.  A block of 16 rows

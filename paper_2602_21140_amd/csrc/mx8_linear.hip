@@ -59,8 +59,8 @@ extern "C" int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales,
                                  revive_stream stream) {
   const char* who = "revive_mx_eight_linear";
   if (activation < REVIVE_ACT_NONE || activation > REVIVE_ACT_GELU) return fail(nullptr, REVIVE_EINVAL, "%s: unknown activation %d", who, activation);
-  if (rows < 0 || rows > (1 << 30) || K <= 0 || K % kMx8Block != 0 || N <= 0 || static_cast<int64_t>(N) * K >= (1ll << 32))
-    return fail(nullptr, REVIVE_EINVAL, "%s: 0 <= rows <= 2^30, N > 0, K a positive multiple of 32 and N * K < 2^32 required", who);
+  if (rows < 0 || rows > (1 << 30) || K <= 0 || K > kMx8MaxK || K % kMx8Block != 0 || N <= 0 || static_cast<int64_t>(N) * K >= (1ll << 32))
+    return fail(nullptr, REVIVE_EINVAL, "%s: 0 <= rows <= 2^30, N > 0, K a positive multiple of 32 up to 2^24 and N * K < 2^32 required", who);
   if (ld_out < N || (residual && ld_residual < N)) return fail(nullptr, REVIVE_EINVAL, "%s: rows at least N elements apart required", who);
   if (residual && residual == out && ld_residual != ld_out) return fail(nullptr, REVIVE_EINVAL, "%s: in place, out and residual have the same distance of rows", who);
   if (rows == 0) return REVIVE_OK;

@@ -199,8 +199,8 @@ int revive_mx_eight_dequantize(const uint8_t* codes, const uint8_t* scales, int6
 
 int revive_mx_eight_packed_bytes(int32_t rows, int32_t K, size_t* bytes) {
   if (!bytes) return fail(nullptr, REVIVE_EINVAL, "revive_mx_eight_packed_bytes: null argument");
-  if (rows <= 0 || K <= 0 || K % kMx8Block != 0 || static_cast<int64_t>(rows) * K >= (1ll << 32))
-    return fail(nullptr, REVIVE_EINVAL, "revive_mx_eight_packed_bytes: rows > 0, K a multiple of 32 and rows * K < 2^32 required");
+  if (rows <= 0 || K <= 0 || K > kMx8MaxK || K % kMx8Block != 0 || static_cast<int64_t>(rows) * K >= (1ll << 32))
+    return fail(nullptr, REVIVE_EINVAL, "revive_mx_eight_packed_bytes: rows > 0, K a multiple of 32 up to 2^24 and rows * K < 2^32 required");
   *bytes = static_cast<size_t>(mx8_packed_bytes(rows, K));
   return REVIVE_OK;
 }

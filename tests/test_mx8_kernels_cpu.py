@@ -52,6 +52,11 @@ def test_host_checks_without_a_gpu():
     L, p = binding.lib(), 1 << 20
     assert L.revive_mx_eight_linear(p, p, 1 << 30, 32, p, 1 << 26, None, 0, None, 0, p, 1 << 26, None) == -1 and b"one launch" in L.revive_last_error(None)
     assert L.revive_mx_eight_linear(p, p, (1 << 30) + 1, 32, p, 32, None, 0, None, 0, p, 32, None) == -1
+    # rows longer than the kernels' 32-bit offsets reach across a tile
+    assert L.revive_mx_eight_linear(p, p, 16, (1 << 24) + 32, p, 7, None, 0, None, 0, p, 7, None) == -1 and b"2^24" in L.revive_last_error(None)
+    with pytest.raises(binding.ReviveError):
+        binding.mx8_packed_bytes(7, (1 << 24) + 32)
+    assert binding.mx8_packed_bytes(7, 1 << 24) == (1 << 24) * 132
     assert L.revive_mx_eight_linear(p, p, 0, 32, p, 32, None, 0, None, 0, p, 32, None) == 0
     assert L.revive_add_rms_norm(p, None, p, 1, 0, 64, 64, 0, 1e-6, None, p, None, None, None) == 0
     assert L.revive_add_rms_norm(p, None, p, 1, 4, 64, 64, 0, 1e-6, p, p + 4096, None, None, None) == -1  # a sum without a residual
@@ -59,3 +64,11 @@ def test_host_checks_without_a_gpu():
     assert binding.mx8_packed_bytes(1, 32) == 128 * 132 and binding.mx8_packed_bytes(129, 160) == 2 * 128 * 2 * 132
     with pytest.raises(binding.ReviveError):
         binding.mx8_packed_bytes(1 << 20, 1 << 12)
+
+
+def test_public_names():
+    import paper_2602_21140_amd as package
+    from paper_2602_21140_amd import binding as calls
+    names = [n for n in vars(package) if n.startswith("mx8_") or n == "add_rms_norm"]
+    assert len(names) == 6 and all(n in package.__all__ and getattr(package, n) is getattr(calls, n) for n in names)
+    assert all(hasattr(package, n) for n in package.__all__)
