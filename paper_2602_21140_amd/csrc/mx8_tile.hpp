@@ -181,8 +181,10 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
       }
   };
 
-  auto run = [&](auto q_tag) {
-    constexpr int Q = decltype(q_tag)::value;  // even: a step ends with the second buffer of activations, and the next one begins with the first
+  // Rows that all are of the first half: the other one is not copied.
+  const bool half = rows <= S::BM / 2;
+  auto run = [&](auto q_tag, auto half_tag) {
+    constexpr int Q = decltype(q_tag)::value, Y = decltype(half_tag)::value ? 0 : CP_Y;  // even: a step ends with the second buffer of activations, and the next one begins with the first
     Mx8Frag af[2][2], bf[TN];
     uint32_t xs[2][2], ws = 0, xw = 0;
     auto read_a = [&](int q, int stage, int x_at, Mx8Frag* f, uint32_t* x) {
@@ -220,8 +222,8 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
       // everybody's.
       auto meet = [&](int clear_half) {
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(MORE ? CP_X + CP_Y : 0));
-        if (!MORE && left && kt == KT - 1 - (clear_half ^ 1)) clear_rest(clear_half ? now : next, clear_half);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(MORE ? CP_X + Y : 0));
+        if (!MORE && left && kt == KT - 1 - (clear_half ^ 1) && (Y || !clear_half)) clear_rest(clear_half ? now : next, clear_half);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       };
@@ -261,12 +263,12 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
           }
           __builtin_amdgcn_sched_barrier(0);  // the registers of these weights take the next step's
           read_b(tn.value, next);
-          if (tn.value < CP_Y) copies(copy_y, tn.value, 1);
+          if (tn.value < Y) copies(copy_y, tn.value, 1);
         });
         pin(std::integral_constant<int, Q - 1>{});
         ws = ws_next;
       } else {
-        copies(copy_y, 0, CP_Y);
+        copies(copy_y, 0, Y);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
@@ -291,18 +293,21 @@ __global__ __launch_bounds__(512, 2) void mx8_tile_kernel(Mx8Args a) {
   for (int kt = 0; kt < min(KT, 2); ++kt) {
 #pragma unroll
     for (int n = 0; n < CP_X; ++n) copy_x(kt, kt, n);
+    if (half) continue;
 #pragma unroll
     for (int n = 0; n < CP_Y; ++n) copy_y(kt, kt, n);
   }
   asm volatile("" ::: "memory");
-  if (KT > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + 2 * CP_Y));  // the first step's weights and first half have landed
+  if (KT > 1 && half) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X));
+  else if (KT > 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(CP_X + 2 * CP_Y));  // the first step's weights and first half have landed
   else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
   if (left && KT == 1) clear_rest(0, 0);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  if (pairs > 2) run(std::integral_constant<int, 4>{});
-  else if (pairs > 0) run(std::integral_constant<int, 2>{});
-  else run(std::integral_constant<int, 0>{});
+  if (pairs > 2) run(std::integral_constant<int, 4>{}, std::false_type{});
+  else if (!half) run(std::integral_constant<int, 2>{}, std::false_type{});
+  else if (pairs > 0) run(std::integral_constant<int, 2>{}, std::true_type{});
+  else run(std::integral_constant<int, 0>{}, std::true_type{});
 
   // A lane holds eight consecutive output columns 8 (l / 16) of activation row l % 16, in each set of 32 columns.  Results leave
   // through LDS, by whole lines.
