@@ -77,47 +77,80 @@ __device__ __forceinline__ Raw<El> load_raw(const El* p) {
   for (int i = 0; i < static_cast<int>(sizeof(El)) / 2; ++i) r.w[i] = mx8_load_any<ONCE>(p + i * (16 / sizeof(El)));
   return r;
 }
-// Units u0, u0 + step, ... of a row of n numbers, zeros past it.  TAIL: n is no multiple of eight; the unit that the row ends in, one
-// lane's, is taken number by number.
-template <typename El, int U, bool ONCE, bool TAIL>
-__device__ __forceinline__ void load_units(Raw<El>* r, const El* row, int u0, int step, int n) {
+// How a row ends: with a whole unit; inside of one, of at least eight numbers; of fewer.
+enum { END_WHOLE, END_INSIDE, END_SHORT };
+
+// Unit u of a row of n numbers, zeros past the row.  END_INSIDE: the unit that the row ends in is the row's last eight numbers, to be
+// moved down by `missing` when they are there: a load that is not waited for, where one of number by number would be (16 384 rows of
+// 2839 bf16 162 us, aligned ones of 2840 88).
+template <typename El, bool ONCE, int END>
+__device__ __forceinline__ Raw<El> load_unit(const El* row, int u, int n) {
+  Raw<El> r;
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    if ((u0 + i * step) * 8 + 8 <= n) r[i] = load_raw<El, ONCE>(row + (u0 + i * step) * 8);
-    else
+  for (int j = 0; j < static_cast<int>(sizeof(El)) / 2; ++j) r.w[j] = mx8_u32x4{0u, 0u, 0u, 0u};
+  if (END == END_SHORT) {
+    uint32_t b[8];
+    mx8_load8<El, false>(row, u * 8, n, b);
 #pragma unroll
-      for (int j = 0; j < static_cast<int>(sizeof(El)) / 2; ++j) r[i].w[j] = mx8_u32x4{0u, 0u, 0u, 0u};
+    for (int i = 0; i < static_cast<int>(sizeof(El)) / 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[i][j] = sizeof(El) == 4 ? b[4 * i + j] : b[2 * j] >> 16 | (b[2 * j + 1] & 0xFFFF0000u);
+  } else if (END == END_WHOLE ? u * 8 + 8 <= n : u * 8 < n) {
+    r = load_raw<El, ONCE>(row + (END == END_WHOLE ? u * 8 : min(u * 8, n - 8)));
   }
-  if (!TAIL) return;
-  const int last = n >> 3, i_last = (last - u0) / step;
-  if (last < u0 || (last - u0) % step != 0 || i_last >= U) return;
-  uint32_t b[8];
-  mx8_load8<El, false>(row, last * 8, n, b);
-  Raw<El> part;
-#pragma unroll
-  for (int i = 0; i < static_cast<int>(sizeof(El)) / 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) part.w[i][j] = sizeof(El) == 4 ? b[4 * i + j] : b[2 * j] >> 16 | (b[2 * j + 1] & 0xFFFF0000u);
-#pragma unroll
-  for (int i = 0; i < U; ++i)
-    if (i == i_last) r[i] = part;
+  return r;
 }
-// The way back, of rounded numbers.
-template <typename El, int U, bool ONCE, bool TAIL>
-__device__ __forceinline__ void store_units(const float (*v)[8], El* row, int u0, int step, int n) {
+__device__ __forceinline__ int missing(int u, int n) { return u * 8 < n ? max(u * 8 + 8 - n, 0) : 0; }
+template <typename El>
+__device__ __forceinline__ void move_down(Raw<El>& r, int by) {
+  constexpr int WORDS = 2 * sizeof(El), HALF = sizeof(El) == 2;
+  uint32_t w[WORDS + 4];
 #pragma unroll
-  for (int i = 0; i < U; ++i)
-    if ((u0 + i * step) * 8 + 8 <= n) mx8_store8<El, ONCE>(row, (u0 + i * step) * 8, 1 << 30, v[i]);
-  if (!TAIL) return;
-  const int last = n >> 3, i_last = (last - u0) / step;
-  if (last < u0 || (last - u0) % step != 0 || i_last >= U) return;
-  float part[8];
+  for (int i = 0; i < WORDS + 4; ++i) w[i] = i < WORDS ? r.w[i / 4][i & 3] : 0u;
 #pragma unroll
-  for (int i = 0; i < U; ++i)
+  for (int bit = 2; bit >= HALF; --bit) {
+    const int words = (1 << bit) >> HALF;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i == i_last) part[j] = v[i][j];
-  mx8_store8<El, false>(row, last * 8, n, part);
+    for (int i = 0; i < WORDS; ++i) w[i] = (by >> bit) & 1 ? (i + words < WORDS ? w[i + words] : 0u) : w[i];
+  }
+  if (HALF) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = by & 1 ? w[i] >> 16 | (i + 1 < WORDS ? w[i + 1] << 16 : 0u) : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) r.w[i / 4][i & 3] = w[i];
+}
+// The way back, of rounded numbers: what is left of a unit in pieces of four, two and one.
+template <typename El, bool ONCE, int END>
+__device__ __forceinline__ void store_unit(const float* v, El* row, int u, int n) {
+  if (u * 8 + 8 <= n) {
+    mx8_store8<El, ONCE>(row, u * 8, 1 << 30, v);
+  } else if (END != END_WHOLE && u * 8 < n) {
+    typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t one __attribute__((aligned(2)));
+    constexpr int WORDS = 2 * sizeof(El);
+    uint32_t w[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = sizeof(El) == 4 ? __float_as_uint(v[i]) : mx8_pack_bf16(v[(2 * i) & 7], v[(2 * i + 1) & 7]);
+    El* p = row + u * 8;
+    if (n & 4) {
+      if (sizeof(El) == 4) mx8_store_any<false>(p, mx8_u32x4{w[0], w[1], w[2], w[3]});
+      else *reinterpret_cast<two*>(p) = two{w[0], w[1]};
+#pragma unroll
+      for (int i = 0; i < WORDS / 2; ++i) w[i] = w[i + WORDS / 2];
+      p += 4;
+    }
+    if (n & 2) {
+      if (sizeof(El) == 4) *reinterpret_cast<two*>(p) = two{w[0], w[1]};
+      else *reinterpret_cast<one*>(p) = w[0];
+      w[0] = w[WORDS / 4];
+      p += 2;
+    }
+    if (n & 1) {
+      if (sizeof(El) == 4) *reinterpret_cast<one*>(p) = w[0];
+      else *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
+    }
+  }
 }
 template <typename El>
 __device__ __forceinline__ float number(const Raw<El>& r, int j) {
@@ -128,7 +161,7 @@ template <typename El>
 __device__ __forceinline__ float rounded(float f) { return sizeof(El) == 4 ? f : __uint_as_float(mx8_pack_bf16(f, f) << 16); }
 
 // s -> y and its 8-bit form, of U units; four neighbouring lanes have a block's.
-template <typename El, int U, bool ONCE, bool TAIL>
+template <typename El, int U, bool ONCE, int END>
 __device__ __forceinline__ void finish(const NormArgs& a, int64_t row, int u0, int step, float (*v)[8], const Raw<El>* weight, double inverse) {
   const int blocks = (a.H + 31) >> 5;
   const float inv = static_cast<float>(inverse);
@@ -141,13 +174,16 @@ __device__ __forceinline__ void finish(const NormArgs& a, int64_t row, int u0, i
     for (int j = 0; j < 8; ++j) {
       const float n = plain ? v[i][j] * inv : static_cast<float>(static_cast<double>(v[i][j]) * inverse);
       v[i][j] = rounded<El>(n * number(weight[i], j));
-      if (TAIL && (u0 + i * step) * 8 + j >= a.H) v[i][j] = 0.f;  // not a NaN of zeros past the row
+      if (END != END_WHOLE && (u0 + i * step) * 8 + j >= a.H) v[i][j] = 0.f;  // not a NaN of zeros past the row
       m = max(m, __float_as_uint(v[i][j]) & 0x7FFFFFFFu);
     }
     byte[i] = mx8_scale_byte(mx8_quad_max(m));
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (a.y) store_units<El, U, ONCE, TAIL>(v, static_cast<El*>(a.y) + row * a.H, u0, step, a.H);
+  if (a.y) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) store_unit<El, ONCE, END>(v[i], static_cast<El*>(a.y) + row * a.H, u0 + i * step, a.H);
+  }
   if (!a.codes) return;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
@@ -165,7 +201,7 @@ __device__ __forceinline__ void finish(const NormArgs& a, int64_t row, int u0, i
 // sum, so that y's last bit, and with it the 8-bit form of a number next to a border, is the same for every shape of the kernel.
 // That costs nothing: what bounds it is HBM, and for few rows the chain of load, sum and store.
 // ONCE (more than the last-level cache holds): numbers past the caches' retention.
-template <typename El, int TPR, int U, bool ONCE, bool TAIL>
+template <typename El, int TPR, int U, bool ONCE, int END>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(NormArgs a) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
   __shared__ double part[2][TPR < 256 ? 1 : TPR / 64];
@@ -174,19 +210,28 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(Nor
   const El* residual = static_cast<const El*>(a.residual);
   Raw<El> rx[U], rr[U], rw[U];
   auto load = [&](int64_t row) {
-    load_units<El, U, ONCE, TAIL>(rx, x + row * a.ld_x, t, TPR, a.H);
-    if (residual) load_units<El, U, ONCE, TAIL>(rr, residual + row * a.ld_residual, t, TPR, a.H);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      rx[i] = load_unit<El, ONCE, END>(x + row * a.ld_x, t + i * TPR, a.H);
+      if (residual) rr[i] = load_unit<El, ONCE, END>(residual + row * a.ld_residual, t + i * TPR, a.H);
+    }
   };
   int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
   const int64_t stride = static_cast<int64_t>(gridDim.x) * ROWS;
   if (row >= a.rows) return;  // with more than one wavefront to a row, the whole workgroup
   load(row);
-  load_units<El, U, false, TAIL>(rw, static_cast<const El*>(a.weight), t, TPR, a.H);
+#pragma unroll
+  for (int i = 0; i < U; ++i) rw[i] = load_unit<El, false, END>(static_cast<const El*>(a.weight), t + i * TPR, a.H);
+  bool first = true;
   for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
     float v[U][8];
     double square = 0;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      if (END == END_INSIDE) {
+        move_down(rx[i], missing(t + i * TPR, a.H));
+        if (residual) move_down(rr[i], missing(t + i * TPR, a.H));
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         v[i][j] = number(rx[i], j);
@@ -195,10 +240,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(Nor
       }
       __builtin_amdgcn_sched_barrier(0);  // or all of the fp64 numbers are made first, and kept
     }
-    if (a.sum) store_units<El, U, ONCE, TAIL>(v, static_cast<El*>(a.sum) + row * a.H, t, TPR, a.H);
+    if (a.sum) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) store_unit<El, ONCE, END>(v[i], static_cast<El*>(a.sum) + row * a.H, t + i * TPR, a.H);
+    }
     if (row + stride < a.rows) load(row + stride);
     const double inverse = inverse_root(row_sum<TPR>(square, part[turn]) / a.H + a.eps);
-    finish<El, U, ONCE, TAIL>(a, row, t, TPR, v, rw, inverse);
+    if (END == END_INSIDE && first) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) move_down(rw[i], missing(t + i * TPR, a.H));
+      first = false;
+    }
+    finish<El, U, ONCE, END>(a, row, t, TPR, v, rw, inverse);
   }
 }
 
@@ -216,8 +269,16 @@ __global__ __launch_bounds__(1024) void add_rms_norm_long_kernel(NormArgs a) {
   float v[U][8];
   auto load = [&](int c) {
     Raw<El> rx[U], rr[U];
-    load_units<El, U, false, true>(rx, x, c + t, TPR, a.H);
-    if (residual) load_units<El, U, false, true>(rr, residual, c + t, TPR, a.H);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      rx[i] = load_unit<El, false, END_INSIDE>(x, c + t + i * TPR, a.H);
+      if (residual) rr[i] = load_unit<El, false, END_INSIDE>(residual, c + t + i * TPR, a.H);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      move_down(rx[i], missing(c + t + i * TPR, a.H));
+      if (residual) move_down(rr[i], missing(c + t + i * TPR, a.H));
+    }
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
@@ -226,9 +287,9 @@ __global__ __launch_bounds__(1024) void add_rms_norm_long_kernel(NormArgs a) {
   double square = 0;
   for (int c = 0; c < units; c += U * TPR) {
     load(c);
-    if (sum) store_units<El, U, false, true>(v, sum, c + t, TPR, a.H);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      if (sum) store_unit<El, false, END_INSIDE>(v[i], sum, c + t + i * TPR, a.H);
 #pragma unroll
       for (int j = 0; j < 8; ++j) square = fma(static_cast<double>(v[i][j]), static_cast<double>(v[i][j]), square);
     }
@@ -238,22 +299,28 @@ __global__ __launch_bounds__(1024) void add_rms_norm_long_kernel(NormArgs a) {
   for (int c = 0; c < units; c += U * TPR) {
     load(c);
     Raw<El> rw[U];
-    load_units<El, U, false, true>(rw, static_cast<const El*>(a.weight), c + t, TPR, a.H);
-    finish<El, U, false, true>(a, row, c + t, TPR, v, rw, inverse);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      rw[i] = load_unit<El, false, END_INSIDE>(static_cast<const El*>(a.weight), c + t + i * TPR, a.H);
+      move_down(rw[i], missing(c + t + i * TPR, a.H));
+    }
+    finish<El, U, false, END_INSIDE>(a, row, c + t, TPR, v, rw, inverse);
   }
 }
 
 constexpr int64_t kOnceBytes = 256ll << 20;
 constexpr int kNormGrid = 2048;  // workgroups that are resident at a time, and more: eight to a CU
 
-template <typename El, int TPR, int U>
+template <typename El, int TPR, int U, bool SHORT = false>
 int launch(const NormArgs& a, hipStream_t stream) {
   constexpr int NT = TPR < 256 ? 256 : TPR;
   const dim3 grid(static_cast<uint32_t>(std::min<int64_t>((a.rows * TPR + NT - 1) / NT, kNormGrid)));
   const bool once = a.rows * a.H * static_cast<int64_t>(sizeof(El)) > kOnceBytes;
-  if (a.H % 8 != 0) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, true>), grid, dim3(NT), 0, stream, a);
-  else if (once) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, true, false>), grid, dim3(NT), 0, stream, a);
-  else hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, false>), grid, dim3(NT), 0, stream, a);
+  if constexpr (SHORT) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, END_SHORT>), grid, dim3(NT), 0, stream, a);
+  else if (a.H % 8 != 0 && once) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, true, END_INSIDE>), grid, dim3(NT), 0, stream, a);
+  else if (a.H % 8 != 0) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, END_INSIDE>), grid, dim3(NT), 0, stream, a);
+  else if (once) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, true, END_WHOLE>), grid, dim3(NT), 0, stream, a);
+  else hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, END_WHOLE>), grid, dim3(NT), 0, stream, a);
   return check_hip(nullptr, hipGetLastError(), "add_rms_norm launch");
 }
 
@@ -281,6 +348,7 @@ int launch_long(const NormArgs& base, hipStream_t stream) {
 template <typename El>
 int launch_norm(const NormArgs& a, hipStream_t s) {
   const int units = ceil_div(a.H, 32) * 4;
+  if (a.H < 8) return launch<El, 64, 1, true>(a, s);
   if (units <= 64) return launch<El, 64, 1>(a, s);
   if (units <= 256) return launch<El, 256, 1>(a, s);
   if (units <= 512) return launch<El, 512, 1>(a, s);
