@@ -166,3 +166,39 @@ def test_library_refuses():
     bad = [*good[:9], 0, 0, 0, 0, None]
     assert L.revive_add_rms_norm(*bad) == -1  # nothing to write
     torch.cuda.synchronize()
+
+
+# rows that end inside of a unit of eight numbers, with every number of them left over, in the lane that ends a wavefront and in
+# the one that begins the next; in place, where the last unit is read beside what another thread writes; more than fits the last-level cache
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H", [9, 10, 11, 12, 13, 14, 15, 509, 514, 1025, 2839, 6151, 8191, 10003, 16383, 16386, 16391])
+def test_rows_that_end_inside_of_a_unit(H, dtype):
+    rows = 2100 if H == 2839 else 5  # more rows than workgroups at a time
+    x, r, w = draw(rows, H, dtype, H)
+    total, y, codes, scales = add_rms_norm(x, w, residual=r, quantize=True)
+    check(x, r, w, 1e-6, total, y, codes, scales)
+    a, b = x.clone(), r.clone()
+    got = add_rms_norm(a, w, residual=b, quantize=True, out=(b, a, torch.empty_like(codes), torch.empty_like(scales)))
+    assert all(torch.equal(g, v) for g, v in zip(got, (total, y, codes, scales)))
+    guarded = torch.full((2, rows * H + 16), 7.0, dtype=dtype, device="cuda")
+    outs = [g[8:8 + rows * H].view(rows, H) for g in guarded]
+    add_rms_norm(x, w, residual=r, out=(*outs, None, None))
+    assert torch.equal(outs[0], total) and torch.equal(outs[1], y)
+    assert bool((guarded[:, :8] == 7.0).all()) and bool((guarded[:, 8 + rows * H:] == 7.0).all())
+    x[2, H - 1], r[3, 0] = float("nan"), -float("inf")
+    got = add_rms_norm(x, w, residual=r, quantize=True)
+    others = [i for i in range(rows) if i not in (2, 3)]
+    assert all(torch.equal(g[others], v[others]) for g, v in zip(got, (total, y, codes, scales)))
+    assert bool(got[1][2].isnan().all()) and bool((got[3][2] == 255).all()) and bool((got[2][2] == 0x7F).all())
+    assert bool(got[1][3, 0].isnan()) and not got[1][3, 1:].any() and int(got[3][3, 0]) == 255 and not got[3][3, 1:].any()
+
+
+@pytest.mark.parametrize("dtype,H", [(torch.bfloat16, 4099), (torch.float32, 2051), (torch.bfloat16, 4096)])
+def test_more_than_the_caches_hold(dtype, H):
+    rows = 33000
+    x, r, w = draw(64, H, dtype, H)
+    many = torch.arange(rows, device="cuda") % 64
+    got = add_rms_norm(x[many], w, residual=r[many], quantize=True)
+    want = add_rms_norm(x, w, residual=r, quantize=True)
+    check(x, r, w, 1e-6, *want)
+    assert all(torch.equal(g, v[many]) for g, v in zip(got, want))
