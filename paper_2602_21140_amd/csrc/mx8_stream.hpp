@@ -16,7 +16,7 @@
 // from HBM there is time for it: 64 tokens on 279 slots of 7168 x 2048 take the same 1.52 ms; a token on 72 slots of 2048 x 1408 24 instead of 22 us,
 // 256 tokens 141 instead of 133.
 //
-// Measured: that FFN of 64 tokens streams its 12.1 GB at 7.1 TB/s at the cases' 1.52 ms; 64 x 7168 x 7168 takes 13 us, 4 TB/s: too short a
+// Measured: that FFN of 64 tokens streams its 10.8 GB at 7.1 TB/s at the cases' 1.52 ms; 64 x 7168 x 7168 takes 13 us, 4 TB/s: too short a
 // stream, of which 3 us are a launch's start and end.
 #pragma once
 
