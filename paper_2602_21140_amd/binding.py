@@ -17,6 +17,7 @@ _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "librevive.so"
 _lib = None
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # private to torch: another one may not have it
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # without the check that CUDA is in use, 0.12 us
 
 SCORE_FN = {"softmax": 0, "sigmoid": 1}
 DTYPE = {"fp32": 0, "bf16": 1}
@@ -357,10 +358,10 @@ def _stream_of(stream, *tensors) -> int:
     without a context launches."""
     device = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (t.get_device() != device or device < 0):
+        if t is not None and t.get_device() != device:
             raise ValueError(f"{tuple(t.shape)} {t.dtype} is on {t.device}: all in the memory of the current device expected")
-    if device != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on device {device}, the current device is {torch.cuda.current_device()}")
+    if device < 0 or device != _get_device():
+        raise ValueError(f"the tensors are on {tensors[0].device}: all in the memory of the current device expected")
     if stream is not None:
         if stream.device_index != device:
             raise ValueError(f"the stream is of device {stream.device_index}, the current device is {device}")
@@ -482,7 +483,7 @@ def mx8_linear(codes: torch.Tensor, scales: torch.Tensor, w: torch.Tensor, n_out
     rows, n = scales.shape
     K = MX_BLOCK * n
     _mx8_check_form(codes, scales, rows, n)
-    n_bytes = mx8_packed_bytes(n_out, K)
+    n_bytes = -(-n_out // 128) * -(-K // 128) * 16896  # mx8_packed_bytes, without the call (0.5 us); the product checks the sizes
     if w.dtype is not torch.uint8 or w.numel() != n_bytes or not w.is_contiguous():
         raise ValueError(f"w {w.dtype} {tuple(w.shape)}: {n_bytes} contiguous bytes of mx8_pack expected")
     _dense(bias, "bias", (n_out,), torch.float32)

@@ -37,7 +37,7 @@ def library(monkeypatch, status):
     calls = {n: status for n in ("revive_add_rms_norm", "revive_mx_eight_quantize", "revive_mx_eight_dequantize", "revive_mx_eight_pack", "revive_mx_eight_linear")}
     monkeypatch.setattr(binding, "lib", lambda: SimpleNamespace(revive_mx_eight_packed_bytes=real.revive_mx_eight_packed_bytes,
                                                             revive_last_error=real.revive_last_error, revive_status_name=real.revive_status_name, **calls))
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_get_device", lambda: 0)
     monkeypatch.setattr(binding, "_raw_stream", lambda device: 0)
 
 
