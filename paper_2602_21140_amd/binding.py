@@ -516,6 +516,8 @@ class ReviveLayer:
         self.L = lib()
         self.cfg = cfg
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:  # the current one, now and when another is current
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.dtype = TORCH_DTYPE[cfg.dtype]
         self.T_max = cfg.T if T_max is None else T_max
         self.P = cfg.n_ranks * cfg.slots_per_rank
