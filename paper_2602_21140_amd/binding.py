@@ -654,6 +654,7 @@ class ReviveLayer:
         for w, n in [(w, n_gu) for w in w_gate_up] + [(w, n_dn) for w in w_down]:
             if w is not None:
                 assert w.dtype == torch.uint8 and w.numel() == n and w.is_contiguous() and w.is_cuda and w.data_ptr() % 16 == 0
+                assert w.get_device() == (self.device.index or 0), f"weights in the memory of {self.device} expected"
         assert all((a is None) == (b is None) for a, b in zip(w_gate_up, w_down)), "a slot has both of its matrices or none"
         I_shared = self.cfg.I_shared
         self._mx8_shared_bytes = (2 * mx8_packed_bytes(I_shared, self.cfg.H), mx8_packed_bytes(self.cfg.H, I_shared)) if I_shared else None

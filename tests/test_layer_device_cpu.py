@@ -24,7 +24,6 @@ def tensors_of(place):
             return place
 
     def make(*shape, dtype=torch.uint8):
-        # from the start of a larger one: 16-byte aligned
         return torch.zeros(*shape, dtype=dtype).as_subclass(There)
     return make
 
@@ -69,3 +68,11 @@ def test_a_layer_on_another_device_than_the_current_one_is_refused(on_device_1):
     layer._mx8_tabs = (torch.zeros(P), torch.zeros(P))
     with pytest.raises(ValueError, match="the layer is on cuda:0"):
         call(layer, tensors_of(1))
+
+
+def test_weights_on_another_device_than_the_layer_are_refused(on_device_1):
+    layer, here, there = ReviveLayer(CFG, device="cuda"), tensors_of(1), tensors_of(0)
+    for gate_up, down in ((there, here), (here, there), (there, there)):
+        with pytest.raises(AssertionError, match="weights in the memory of cuda:1"):
+            layer.set_mx8_expert_weights([here(GATE_UP), None, gate_up(GATE_UP)], [here(DOWN), None, down(DOWN)])
+    layer.set_mx8_expert_weights([here(GATE_UP), None, None], [here(DOWN), None, None])
