@@ -35,7 +35,7 @@ constexpr size_t mx8_stream_lds() {
 
 // WIDE: rows of A that are reached by 64 bits (otherwise all of A, or of a dense problem's tile, is within 4 GiB).
 template <int TMX, int W, int NW, int D, int EPI, bool WIDE>
-__global__ __launch_bounds__(64 * NW, (NW > 8 ? 4 : 2)) void mx8_stream_kernel(Mx8Args a) {
+__global__ __launch_bounds__(64 * NW, 2) void mx8_stream_kernel(Mx8Args a) {
   static_assert(W % 2 == 0 && W <= 4 && (EPI != EPI8_H || W == 4) && NW > 1, "output columns in sets of 32, sums by way of LDS");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const bool dense = blockIdx.x < static_cast<unsigned>(a.dense.blocks);
@@ -263,8 +263,8 @@ int launch_mx8_stream(const revive_ctx* ctx, const Mx8Args& args, hipStream_t st
   const int grid = args.dense.blocks + args.grouped.blocks;
   if (grid <= 0) return REVIVE_OK;
   constexpr size_t lds = mx8_stream_lds<TMX, W, NW>();
+  static_assert(lds <= 64 * 1024, "what a kernel has without asking for more");
   auto kern = mx8_stream_kernel<TMX, W, NW, D, EPI, WIDE>;
-  if (lds > 64 * 1024) REVIVE_HIP(ctx, allow_dynamic_lds(reinterpret_cast<const void*>(kern), lds));
   hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * NW), lds, stream, args);
   return check_hip(ctx, hipGetLastError(), "mx8_stream launch");
 }
