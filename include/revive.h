@@ -411,7 +411,8 @@ int revive_mx_expert_ffn(revive_ctx* ctx, const void* x, const int32_t* src_of, 
  *           up with zeros
  *   scales  dev uint8 [rows, ceil(K/32)]
  * revive_mx_eight_dequantize: the numbers they stand for, [rows, K], rows ld elements apart;
- *   fp32 holds them exactly, bf16 those of 2^-133 and above (others are rounded to it).
+ *   fp32 holds them exactly below 2^128, bf16 from 2^-133 on, too (others are rounded: to
+ *   infinity at the upper end, where only a number from 31/32 * 2^128 on is rounded).
  * K <= 2^24.  Rows may start at any address that fits their elements. */
 int revive_mx_eight_quantize(const void* x, int32_t dtype, int64_t rows, int32_t K, int64_t ld, uint8_t* codes,
                         uint8_t* scales, revive_stream stream);
@@ -478,8 +479,9 @@ int revive_mx_eight_linear(const uint8_t* x, const uint8_t* x_scales, int32_t ro
  * rounding above along a row, for every slot p with rows [slot_offsets[p],
  * slot_offsets[p+1]):  h = Q(silu(x G_p) * (x U_p)),  y = h D_p, and the same on all T rows
  * of x for the shared expert when y_shared != NULL.  Sums as of the product above; those
- * behind h are exact fp32 where there are few rows or few numbers of h, so that a token's
- * result goes by T too, by an h that is rounded to the code beside.
+ * behind h are fp32 sums of bf16 products where there are few rows or few numbers of h
+ * (operands below 2^-126 have fewer bits there, and those of 2^128 are infinities), so that
+ * a token's result goes by T too, by an h that is rounded to the code beside.
  *   x, x_scales  dev: the tokens' codes [T, H], 16-byte aligned, and scales [T, H/32], not
  *              permuted (revive_add_rms_norm, revive_mx_eight_quantize)
  *   src_of     dev int32 [N] (revive_dispatch_index): row r is token src_of[r] / k

@@ -19,12 +19,14 @@ namespace {
 // 32 rows at a time) streamed and by tiles: 288 slots, H = 7168, I = 2048: 7 rows 1881 1954, 1877 1950, 25 rows 2318 2343, 2366 2391, 39 rows
 // 2700 2430, 2710 2660; 72 slots, H = 2048, I = 1408: 18 rows 127 124, 126 136, 27 rows 147 131, 147 155, 43 rows 172 139, 166 167, 84 rows 285
 // 190, 275 254.  The host knows no row counts: the average is over all slots, without rows or not.  Fewer tiles than kMx8TileGrid
-// leave too many CUs without one.
+// leave too many CUs without one.  The shared expert takes the form of the routed rows, but for the case below: beside few of them all of its
+// rows are streamed (288 slots, 2048 x 256, one slot a token, I_shared = 2816: 6000 tokens 378 us, 141 without the shared expert, 8000 tokens 319).
 constexpr int kMx8TileRowsGateUp = 24, kMx8TileRowsDown = 36, kMx8TileGrid = 96;
-// The tiles' sums of gate and up are those of the 8-bit instruction (mx8_product.hpp), after which some 6 of 10 000 numbers of h are
-// rounded to the neighbouring code: y's relative error is 0.0020 so, 0.0017 of it bf16's rounding, if there are many numbers to
-// even that out; of 400 000 numbers it was up to 0.0027.  Fewer than 2^20 numbers are left to the streaming kernel, whose sums
-// are exact, the shared expert's in a launch of their own if the routed ones are many.
+// The tiles' sums of gate and up are those of the 8-bit instruction (mx8_product.hpp), after which some 17 of 10 000 numbers of h are
+// rounded to another code (H = 256 to 2048; h is off by 0.0010 to 0.0012 of its size): y's relative error is 0.0020 so, 0.0017 of it bf16's
+// rounding, if there are many numbers to even that out; of 400 000 numbers it was up to 0.0027.  Fewer than 2^20 numbers are left to the
+// streaming kernel, whose sums are fp32 (of 500 000 numbers none is rounded to another code), the shared expert's in a launch of their own
+// if the routed ones are many.
 constexpr int64_t kMx8ManyNumbers = 1 << 20;
 
 struct Mx8Ffn {

@@ -36,6 +36,11 @@ int linear_tile(const Mx8Problem& base, hipStream_t stream) {
 // 1003 rows, K = 2048, N = 1411 37 25 13 14; 64 rows, K = 16384, N = 576 - - 42 21 17 12.5.
 // So the tiles through LDS, which multiply fastest, where they give half of the CUs one, those of 128 columns as long as none gets
 // two; else the largest form that gives nearly every CU one.
+// Between 112 and 223 workgroups the larger of two forms is the faster one as well, and this rule passes over it.  K = 7168, 32 x 64 (144, 160,
+// 192, 220, 224 workgroups), 16 x 64 (twice as many), 64 rows: N = 4608 12.4 17.8, 5120 12.5 17.9, 6144 12.9 18.2, 7040 13.5 18.6, 7168 13.5 18.3; 16 x 64 (as
+// many), 16 x 32 (twice as many), 32 rows: 10.5 13.1, 10.7 13.3, 11.0 13.6, 11.7 14.0, 11.5 13.8; 64 x 64 (144 to 224), 32 x 64, 128 rows: 16.8 18.7, 17.0 19.0, 17.4
+// 19.2, 17.3 19.8, 17.3 19.3.  A second workgroup on some of the CUs is what costs: up to 256 of them the smaller form wins (48 rows, 16 x 64 and 32 x 64:
+// N = 4608, 216 workgroups, 10.6 12.1, N = 6144, 288, 18.0 12.5).
 constexpr int kMx8Cus = 256, kMx8HalfGrid = 128, kMx8FullGrid = 224;
 
 int linear(const Mx8Problem& p, hipStream_t s) {

@@ -10,8 +10,8 @@
 // own (as operands straight from memory, 16 rows of 64 bytes, a product of 64 rows takes twice as long).  Their scales come for
 // 16 steps at once.
 //
-// EPI8_H multiplies in bf16, which holds both operands' numbers, scales included, and whose products are added up in fp32.  An
-// h that is off by the 3e-5 of the 8-bit instruction is rounded to the next code, 2^-4 away, some 6 times in 10 000: with few rows
+// EPI8_H multiplies in bf16, which holds both operands' numbers, scales included (from 2^-126 on, below 2^128), and whose products are added up
+// in fp32.  An h that is off by the 3e-5 of the 8-bit instruction is rounded to another code, 2^-4 away, some 17 times in 10 000: with few rows
 // a single one of them shows (y of 8 rows, I = 896: relative error 0.0030, of which bf16's rounding is 0.0017).  While weights come
 // from HBM there is time for it: 64 tokens on 279 slots of 7168 x 2048 take the same 1.52 ms; a token on 72 slots of 2048 x 1408 24 instead of 22 us,
 // 256 tokens 141 instead of 133.

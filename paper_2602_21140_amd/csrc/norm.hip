@@ -257,7 +257,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rms_norm_kernel(Nor
 }
 
 // Rows that do not fit a workgroup's registers are read twice: by way of `sum` the second time, where there is one (x or the residual
-// may be what it replaces).
+// may be what it replaces).  HBM bounds it, and the second reading where the caches have not kept the row: with residual and 8-bit form,
+// counted once, 16 384 rows of 8200 fp32 numbers 526 us, 4.4 TB/s (8192, read once: 438 us, 5.2), 10 000 of 12 000 442 us, 4.6, 8000 of 16 384 444 us,
+// 5.0; bf16, 8000 rows of 20 000 313 us, 4.6 (16 384, read once: 223 us, 5.3).
 template <typename El>
 __global__ __launch_bounds__(1024) void add_rms_norm_long_kernel(NormArgs a) {
   constexpr int U = 2, TPR = 1024;
@@ -318,7 +320,8 @@ int launch(const NormArgs& a, hipStream_t stream) {
   const dim3 grid(static_cast<uint32_t>(std::min<int64_t>((a.rows * TPR + NT - 1) / NT, kNormGrid)));
   const bool once = a.rows * a.H * static_cast<int64_t>(sizeof(El)) > kOnceBytes;
   if constexpr (SHORT) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, END_SHORT>), grid, dim3(NT), 0, stream, a);
-  // rows at any address, past the caches' retention or not: 32 768 x 5001 bf16 494 and 515 us, 20 000 x 4001 fp32 290 and 264
+  // rows at any address, past the caches' retention or not: 32 768 x 5001 bf16 494 and 515 us (3.0 TB/s; 32 768 x 5000
+  // aligned 305 us, 4.9), 20 000 x 4001 fp32 290 and 264
   else if (a.H % 8 != 0 && once && sizeof(El) == 2) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, sizeof(El) == 2, END_INSIDE>), grid, dim3(NT), 0, stream, a);
   else if (a.H % 8 != 0) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, false, END_INSIDE>), grid, dim3(NT), 0, stream, a);
   else if (once) hipLaunchKernelGGL((add_rms_norm_kernel<El, TPR, U, true, END_WHOLE>), grid, dim3(NT), 0, stream, a);
@@ -346,7 +349,8 @@ int launch_long(const NormArgs& base, hipStream_t stream) {
 
 // A unit a thread as long as a workgroup can hold the row: us of 1024 threads with one unit and 256 with four, bf16 with residual
 // and 8-bit output, H = 7168: 64 rows 4.8 (256 threads, weights loaded after the sum: 8.1), 1003 rows 16.8 and 16.2, 4096 rows 62 and
-// 57, 32 768 rows 392 (5.4 TB/s) and 413.  
+// 57, 32 768 rows 392 (5.4 TB/s) and 413.  Between the forms' lengths
+// threads are without a unit, 188 of 256 at 513 numbers: 8000 rows of these take 20.3 us (1.8 TB/s), of 1024 numbers 19.4.
 template <typename El>
 int launch_norm(const NormArgs& a, hipStream_t s) {
   const int units = ceil_div(a.H, 32) * 4;
